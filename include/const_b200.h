@@ -44,7 +44,8 @@ typedef enum {
     CONST_ERR_TIMEOUT = 8           /* a bounded device-side wait gave up                              */
 } const_status_t;
 
-typedef enum { CONST_F32 = 0, CONST_F64 = 1 } const_dtype_t;
+/* CONST_BF16 is a type of factors and gradients in const_softmax_loss and const_clip_gradients alone. */
+typedef enum { CONST_F32 = 0, CONST_F64 = 1, CONST_BF16 = 2 } const_dtype_t;
 
 typedef struct const_csf const_csf_t;     /* opaque: a sparse tensor in CSF form, on the device */
 typedef struct const_plan const_plan_t;   /* opaque: a checked schedule bound to a kernel family */
@@ -257,6 +258,49 @@ const char *const_plan_family(const const_plan_t *plan);
  */
 const_status_t const_execute(const_plan_t *plan, const const_operand_t *operands, int n_operands,
                              void *out_dev, void *stream);
+
+/*
+ * Softmax cross entropy over the leaf mode of a CSF tensor, with its gradient.  (The paper stops at the contractions; this
+ * is the loss that a CP model of such a tensor is trained with, MTTKRP being the gradient of its data term.)
+ *
+ * Rows are the fibres f of `csf` (order 2..4, CONST_F32): the nodes of the level above the leaves, in CSF order.  With one
+ * factor per mode, `rank` columns each, h_f the elementwise product of the factor rows on the fibre's path and c_k the rows
+ * of the leaf mode's factor, the score of coordinate k is s_fk = <h_f, c_k>, for every k of the leaf mode.  The stored leaves
+ * x_fk are the targets and their weights:
+ *     loss_f = w_f log sum_k exp s_fk - sum_leaves x_fk s_fk,      w_f = sum_leaves x_fk.
+ * Of order 2 this is the loss of a language model's head: rows of hidden states, a table of the vocabulary, one leaf a row; a row
+ * that no leaf is stored for takes no part (its gradient is zero).
+ *
+ *   factors_dev   one per mode (not per level), row-major [extent of the mode][rank], CONST_F32 or CONST_BF16 (factor_dtype);
+ *   loss_dev      float, one per fibre (const_csf_level(order - 2) says how many), overwritten;
+ *   grads_dev     NULL: the loss alone.  Else one per mode, each NULL (not wanted) or an array like that factor, which
+ *                 is overwritten with the gradient of scale * sum_f loss_f.  No two of them, nor one of them and a factor, overlap.
+ * The scores are never stored: they are made tile by tile, twice where there is a gradient.  Scores, maxima, sums and gradients
+ * are held in fp32; bf16 gradients are rounded once at the end.  Scores that are not finite make the losses of their rows,
+ * and the gradients that these rows reach, not finite.  Gradients are added up with atomic adds, so they can differ in the
+ * last bits between runs; losses do not, except of fibres with more than 64 leaves.
+ * Scratch comes from the library's pool as for const_execute (rows, their weights, partial sums; no array of the size
+ * fibres x extent); without it the call returns CONST_ERR_CUDA and has written nothing.  Asynchronous on `stream`, no host
+ * synchronisation; may be captured into a graph.  The current device has to be the tensor's.
+ * CONST_ERR_INVALID_ARG: null or not 16-byte aligned pointers, a csf or a type other than these, rank < 1, a scale that is
+ * not finite.  CONST_ERR_UNSUPPORTED: rank > 1024.
+ */
+const_status_t const_softmax_loss(const const_csf_t *csf, const void *const *factors_dev, int rank, const_dtype_t factor_dtype,
+                                  double scale, void *loss_dev, void *const *grads_dev, void *stream);
+
+/*
+ * The global norm of n gradients, and the gradients scaled so that it is at most max_norm:
+ *     norm = sqrt(sum of the squares of all values of all tensors),   out = grad * min(1, max_norm / norm).
+ * grads_dev[i] holds sizes[i] values (0 is allowed) of `dtype` (CONST_F32, CONST_F64 or CONST_BF16) at any address that is a
+ * multiple of one value; 16-byte aligned ones are read and written with 128-bit accesses.  out_dev NULL, or an entry equal to that of grads_dev:
+ * in place; otherwise the arrays must not overlap any other.  norm_dev receives the norm before the scaling (float; double for CONST_F64).
+ * max_norm >= 0; infinity scales nothing.  A norm that is not finite scales nothing either: the values come through
+ * as they are, and the caller sees the norm and drops the step.
+ * Squares are added in fp32 over at most 8 values and in fp64 above that, in an order that only the sizes decide: the same call
+ * gives the same bits.  Scratch (some 10 KB) as for const_execute; without it CONST_ERR_CUDA.  Asynchronous on `stream`; may be captured.
+ */
+const_status_t const_clip_gradients(int n, const void *const *grads_dev, void *const *out_dev, const int64_t *sizes,
+                                    const_dtype_t dtype, double max_norm, void *norm_dev, void *stream);
 
 /*
  * Concrete index notation of a schedule (Sec. 4.2, Algorithm 1 `generate` with its helper `remove`):

@@ -14,7 +14,7 @@ from typing import Dict, List, Optional, Sequence, Tuple, Union
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libconst_b200.so"
 
-F32, F64 = 0, 1
+F32, F64, BF16 = 0, 1, 2
 STATUS_NAMES = {0: "CONST_OK", 1: "CONST_ERR_INVALID_ARG", 2: "CONST_ERR_UNSUPPORTED",
                 3: "CONST_ERR_ILLEGAL_SCHEDULE", 4: "CONST_ERR_DUPLICATE_COORD", 5: "CONST_ERR_COORD_RANGE",
                 6: "CONST_ERR_WORKSPACE", 7: "CONST_ERR_CUDA", 8: "CONST_ERR_TIMEOUT"}
@@ -94,6 +94,10 @@ def load_library():
     lib.const_plan_describe.restype = i32
     lib.const_plan_set_generic_executor.argtypes = [vp, i32]
     lib.const_plan_set_generic_executor.restype = i32
+    lib.const_softmax_loss.argtypes = [vp, pp(vp), i32, i32, ctypes.c_double, vp, pp(vp), vp]
+    lib.const_softmax_loss.restype = i32
+    lib.const_clip_gradients.argtypes = [i32, pp(vp), pp(vp), pp(i64), i32, ctypes.c_double, vp, vp]
+    lib.const_clip_gradients.restype = i32
     lib.const_destroy.argtypes = [vp]
     lib.const_destroy.restype = None
     lib.const_profile_enable.argtypes = [i32]
@@ -138,10 +142,12 @@ def _stream_ptr(stream) -> ctypes.c_void_p:
 
 
 class CsfHandle:
-    """Owns a const_csf_t*; `order`, `dtype`, `stream` mirror the build arguments."""
+    """Owns a const_csf_t*; `order`, `dtype`, `stream`, `dims`, `mode_order` mirror the build arguments."""
 
-    def __init__(self, ptr: int, order: int, dtype: int, stream: Optional[int] = None):
+    def __init__(self, ptr: int, order: int, dtype: int, stream: Optional[int] = None, dims: Sequence[int] = (),
+                 mode_order: Sequence[int] = ()):
         self.ptr, self.order, self.dtype, self.stream = ptr, order, dtype, stream
+        self.dims, self.mode_order = tuple(int(d) for d in dims), tuple(int(m) for m in mode_order)
 
     def __del__(self):
         try:
@@ -182,7 +188,7 @@ def const_csf_build(coords, vals, dims: Sequence[int], mode_order: Sequence[int]
     on = _stream_int(stream)
     st = lib.const_csf_build(order, dims_a, nnz, cptr, vals.data_ptr(), dtype, mo_a, on, ctypes.byref(out))
     _check(st, "const_csf_build")
-    return CsfHandle(out.value, order, dtype, on)
+    return CsfHandle(out.value, order, dtype, on, dims, mode_order)
 
 
 def const_csf_from_dense(dense, mode_order: Sequence[int], stream=None) -> CsfHandle:
@@ -198,7 +204,7 @@ def const_csf_from_dense(dense, mode_order: Sequence[int], stream=None) -> CsfHa
     out = ctypes.c_void_p()
     on = _stream_int(stream)
     _check(lib.const_csf_from_dense(order, dims_a, dense.data_ptr(), dtype, mo_a, on, ctypes.byref(out)), "const_csf_from_dense")
-    return CsfHandle(out.value, order, dtype, on)
+    return CsfHandle(out.value, order, dtype, on, dense.shape, mode_order)
 
 
 def const_csf_build_noalloc(coords, vals, dims: Sequence[int], mode_order: Sequence[int], pos_out, crd_out,
@@ -406,6 +412,77 @@ def const_execute(plan: PlanHandle, operands: Dict[str, Union[CsfHandle, "object
         raise ValueError("output must be a contiguous CUDA tensor")
     n = len(ops)
     _check(lib.const_execute(plan.ptr, _operand_array(n)(*ops), n, out.data_ptr(), _stream_int(stream)), "const_execute")
+
+
+_torch_dtypes = None
+
+
+def _dtype_of(tensor, types) -> int:
+    global _torch_dtypes
+    if _torch_dtypes is None:
+        import torch
+        _torch_dtypes = {torch.float32: F32, torch.float64: F64, torch.bfloat16: BF16}
+    found = _torch_dtypes.get(tensor.dtype)
+    if found not in types:
+        raise ValueError(f"values of type {tensor.dtype} are not taken here")
+    return found
+
+
+def const_softmax_loss(csf: CsfHandle, factors, loss, grads=None, scale: float = 1.0, stream=None) -> None:
+    """Softmax cross entropy over the leaf mode of `csf`, one loss a fibre, with the factors' gradients (see the header).
+
+    factors: one float32 or bfloat16 CUDA tensor [extent, rank] per mode; loss: float32 CUDA tensor, one entry a fibre.
+    grads: None (the loss alone), or per mode None or a tensor like the factor.  `loss` and `grads` are overwritten.
+    """
+    lib = _lib or load_library()
+    order = csf.order
+    if len(factors) != order or (grads is not None and len(grads) != order):
+        raise ValueError("factors and grads must have one entry per mode")
+    kind = _dtype_of(factors[0], (F32, BF16))
+    rank = int(factors[0].shape[-1])
+    for m, f in enumerate(factors):
+        for what, t in (("factor", f), ("gradient", None if grads is None else grads[m])):
+            if t is None and what == "gradient":
+                continue
+            if not t.is_cuda or not t.is_contiguous() or t.dtype != factors[0].dtype or tuple(t.shape) != (csf.dims[m], rank):
+                raise ValueError(f"{what} {m} must be a contiguous {factors[0].dtype} CUDA tensor of shape {(csf.dims[m], rank)}")
+    n = ctypes.c_int64()
+    _check(lib.const_csf_level(csf.ptr, order - 2, None, None, ctypes.byref(n)), "const_csf_level")
+    if not loss.is_cuda or not loss.is_contiguous() or _dtype_of(loss, (F32,)) != F32 or loss.numel() != n.value:
+        raise ValueError(f"loss must be a contiguous float32 CUDA tensor of {n.value} entries, one a fibre")
+    if n.value == 0 and grads is None:
+        return
+    ptrs = (ctypes.c_void_p * order)(*[f.data_ptr() for f in factors])
+    outs = None if grads is None else (ctypes.c_void_p * order)(*[None if g is None else g.data_ptr() for g in grads])
+    at = loss.data_ptr() if n.value else factors[0].data_ptr()          # torch gives an empty tensor no address; nothing is written there
+    _check(lib.const_softmax_loss(csf.ptr, ptrs, rank, kind, float(scale), at, outs, _stream_int(stream)), "const_softmax_loss")
+
+
+def const_clip_gradients(grads, max_norm: float, norm, out=None, stream=None) -> None:
+    """Scales `grads` (CUDA tensors of one type: float32, float64 or bfloat16) so that their global norm is at most max_norm.
+
+    norm: CUDA tensor of one value (float32; float64 for float64 gradients), receives the norm before the scaling.
+    out: None (in place), or one tensor like each of `grads`.  A norm that is not finite scales nothing.
+    """
+    import torch
+    lib = _lib or load_library()
+    n = len(grads)
+    kind = _dtype_of(grads[0], (F32, F64, BF16)) if n else F32
+    outs = grads if out is None else out
+    if len(outs) != n:
+        raise ValueError("out must have one entry per gradient")
+    for g, o in zip(grads, outs):
+        if not g.is_cuda or not g.is_contiguous() or g.dtype != grads[0].dtype:
+            raise ValueError("gradients must be contiguous CUDA tensors of one type")
+        if o is not g and (not o.is_cuda or not o.is_contiguous() or o.dtype != g.dtype or o.shape != g.shape):
+            raise ValueError("out must hold tensors like the gradients")
+    if not norm.is_cuda or norm.numel() != 1 or norm.dtype != (torch.float64 if kind == F64 else torch.float32):
+        raise ValueError("norm must be a CUDA tensor of one float32 (float64 for float64 gradients)")
+    src = (ctypes.c_void_p * max(n, 1))(*[g.data_ptr() for g in grads])
+    dst = None if out is None else (ctypes.c_void_p * max(n, 1))(*[o.data_ptr() for o in outs])
+    sizes = (ctypes.c_int64 * max(n, 1))(*[g.numel() for g in grads])
+    _check(lib.const_clip_gradients(n, src, dst, sizes, kind, float(max_norm), norm.data_ptr(), _stream_int(stream)),
+           "const_clip_gradients")
 
 
 def const_plan_set_tensor_stage(plan: PlanHandle, enable: bool) -> None:

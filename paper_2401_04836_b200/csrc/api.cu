@@ -1,6 +1,7 @@
 // C-ABI entry points (include/const_b200.h): argument checking, handle management, dispatch.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstring>
 #include <new>
 
@@ -370,6 +371,45 @@ const_status_t const_execute(const_plan_t *h, const const_operand_t *operands, i
         default:
             return CONST_ERR_UNSUPPORTED;
     }
+}
+
+const_status_t const_softmax_loss(const const_csf_t *h, const void *const *factors_dev, int rank, const_dtype_t factor_dtype, double scale,
+                                  void *loss_dev, void *const *grads_dev, void *stream) {
+    const const_csf *c = as_csf(h);
+    if (!c || !factors_dev || !loss_dev || (factor_dtype != CONST_F32 && factor_dtype != CONST_BF16) || c->dtype != CONST_F32 || rank < 1 ||
+        !std::isfinite((float)scale))
+        return CONST_ERR_INVALID_ARG;
+    if (!aligned16(loss_dev)) return CONST_ERR_INVALID_ARG;
+    for (int m = 0; m < c->order; ++m) {
+        if (!factors_dev[m] || !aligned16(factors_dev[m])) return CONST_ERR_INVALID_ARG;
+        if (!grads_dev || !grads_dev[m]) continue;
+        if (!aligned16(grads_dev[m])) return CONST_ERR_INVALID_ARG;
+        for (int o = 0; o < c->order; ++o)                      // a gradient is cleared before the factors are read
+            if (grads_dev[m] == factors_dev[o] || (o != m && grads_dev[m] == grads_dev[o])) return CONST_ERR_INVALID_ARG;
+    }
+    if (rank > kMaxLossRank) return CONST_ERR_UNSUPPORTED;
+    int dev = 0;
+    CB_CUDA(cudaGetDevice(&dev));
+    if (dev != c->device) return CONST_ERR_INVALID_ARG;
+    return run_softmax_loss(c, factors_dev, rank, factor_dtype, (float)scale, static_cast<float *>(loss_dev), grads_dev,
+                            static_cast<cudaStream_t>(stream));
+}
+
+const_status_t const_clip_gradients(int n, const void *const *grads_dev, void *const *out_dev, const int64_t *sizes, const_dtype_t dtype,
+                                    double max_norm, void *norm_dev, void *stream) {
+    if (n < 0 || (n > 0 && (!grads_dev || !sizes)) || !norm_dev || !(max_norm >= 0.0) ||
+        (dtype != CONST_F32 && dtype != CONST_F64 && dtype != CONST_BF16))
+        return CONST_ERR_INVALID_ARG;
+    const uintptr_t width = dtype == CONST_F64 ? 8 : dtype == CONST_F32 ? 4 : 2, result = dtype == CONST_F64 ? 8 : 4;
+    if (reinterpret_cast<uintptr_t>(norm_dev) % result) return CONST_ERR_INVALID_ARG;
+    if (!out_dev) out_dev = const_cast<void *const *>(reinterpret_cast<const void *const *>(grads_dev));
+    for (int i = 0; i < n; ++i) {
+        if (sizes[i] < 0) return CONST_ERR_INVALID_ARG;
+        if (sizes[i] == 0) continue;
+        if (!grads_dev[i] || !out_dev[i] || reinterpret_cast<uintptr_t>(grads_dev[i]) % width || reinterpret_cast<uintptr_t>(out_dev[i]) % width)
+            return CONST_ERR_INVALID_ARG;
+    }
+    return run_clip_gradients(n, grads_dev, out_dev, sizes, dtype, max_norm, norm_dev, static_cast<cudaStream_t>(stream));
 }
 
 const_status_t const_plan_set_tensor_stage(const_plan_t *h, int enable) {

@@ -15,6 +15,7 @@ namespace cb {
 constexpr uint32_t kCsfMagic = 0x31465343u;   // "CSF1"
 constexpr uint32_t kPlanMagic = 0x314e4c50u;  // "PLN1"
 constexpr int kMaxOrder = 4;
+constexpr int kMaxLossRank = 1024;            // of const_softmax_loss
 
 // One thread-block work item of the fused kernels.
 //   kind 0: a group of light slices, one per warp: `slice` = first index into the light list, f0 = how many
@@ -218,6 +219,12 @@ const_status_t run_network(const const_csf *U, const double *V, const const_csf 
 const_status_t run_network_dense(const const_csf *U, const double *V, const const_csf *W, double *Z, int64_t n_i, int64_t n_j,
                                  int64_t n_k, int64_t n_l, int64_t n_m, int32_t **mode_out, void **scratch_out, cudaStream_t stream);
 
+// softmax_loss.cu: factors and gradients by mode (X in fp32; grads, and any of them, may be null)
+const_status_t run_softmax_loss(const const_csf *X, const void *const *factors, int rank, const_dtype_t dtype, float scale, float *out,
+                                void *const *grads, cudaStream_t stream);
+// clip_gradients.cu
+const_status_t run_clip_gradients(int count, const void *const *in, void *const *out, const int64_t *sizes, const_dtype_t dtype, double max_norm,
+                                  void *norm, cudaStream_t stream);
 // tree_kernel.cu: the generic executor; sparse[slot] and global_in[slot] follow cp.sparse_names / cp.global_names
 const_status_t run_tree(const tree::Compiled &cp, const_dtype_t dtype, const const_csf *const *sparse,
                         void *const *global_in, void *out_dev, cudaStream_t stream);

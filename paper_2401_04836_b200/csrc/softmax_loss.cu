@@ -1,0 +1,487 @@
+// Softmax cross entropy over the leaf mode of a CSF tensor, with its gradient: the steps around the two passes over the
+// scores, the passes on the fp32 pipes, and the host side.  (softmax_loss.cuh has the mathematics.)
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "softmax_loss.cuh"
+
+namespace cb {
+namespace loss {
+namespace {
+
+constexpr int kWarp = 32;
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / kWarp;
+constexpr int kRun = 64;           // leaves of a warp's run
+constexpr int kStrip = 128;        // columns of a row that a warp holds at once, 4 a lane
+
+__device__ __forceinline__ float value(const float *p, int64_t i) { return __ldg(p + i); }
+__device__ __forceinline__ float value(const __nv_bfloat16 *p, int64_t i) { return __bfloat162float(p[i]); }
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The last p in [0, n) with pos[p] <= at (pos ascends; every node has a child, so it is the node that holds `at`).
+__device__ __forceinline__ int32_t holder(const int32_t *__restrict__ pos, int64_t n, int64_t at) {
+    int64_t lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) >> 1;
+        if (__ldg(pos + mid) <= at) lo = mid; else hi = mid - 1;
+    }
+    return (int32_t)lo;
+}
+
+// Zeroes what is added to: accumulators of the gradients and the sums over leaves.
+struct Zero {
+    float *at[kMaxOrder + 1];
+    int64_t n[kMaxOrder + 1];
+};
+__global__ void __launch_bounds__(kThreads) loss_clear(Zero z) {
+    after_last_kernel();
+    start_next_kernel();
+    const int64_t me = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
+#pragma unroll
+    for (int a = 0; a <= kMaxOrder; ++a) {
+        const int64_t quads = z.n[a] / 4;                          // every start is 16-byte aligned
+        for (int64_t i = me; i < quads; i += all) reinterpret_cast<float4 *>(z.at[a])[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int64_t i = 4 * quads + me; i < z.n[a]; i += all) z.at[a][i] = 0.f;
+    }
+}
+
+// h_f of the fibre with path `at`, element r
+template <typename T>
+__device__ __forceinline__ float row_value(const Problem &p, const int32_t *at, int r) {
+    float h = value(static_cast<const T *>(p.factor[0]), (int64_t)at[0] * p.rank + r);
+    for (int l = 1; l + 1 < p.order; ++l) h *= value(static_cast<const T *>(p.factor[l]), (int64_t)at[l] * p.rank + r);
+    return h;
+}
+
+__device__ __forceinline__ void path_of(const Problem &p, int64_t f, int32_t *at) {
+    int64_t node = f;
+    for (int l = p.order - 2; l >= 0; --l) {
+        at[l] = __ldg(p.crd[l] + node);
+        if (l > 0) node = holder(p.pos[l], p.nodes[l - 1], node);
+    }
+}
+
+// One warp a fibre: its path and its row h.
+template <typename T>
+__device__ __forceinline__ void make_row(const Problem &p, int64_t f) {
+    const int lane = threadIdx.x % kWarp;
+    int32_t at[kMaxOrder - 1];
+    path_of(p, f, at);
+    for (int l = lane; l + 1 < p.order; l += kWarp) p.path[l][f] = at[l];
+    for (int r = lane; r < p.rank; r += kWarp) p.h[f * p.rank + r] = row_value<T>(p, at, r);
+}
+
+// One warp a run of kRun leaves, whatever fibres they lie in: weights, target scores and, with a gradient, the targets' share of
+// it.  A fibre's sums leave the registers when the run leaves the fibre; only a fibre that is cut by the ends of runs gets
+// more than one addition.
+template <typename T>
+__device__ __forceinline__ void walk_leaves(const Problem &p, int64_t first, int64_t last, bool grad) {
+    const int lane = threadIdx.x % kWarp;
+    const int fl = p.order - 2;                                      // level of the fibres
+    const int32_t *__restrict__ ends = p.pos[fl + 1];
+    const T *table = static_cast<const T *>(p.factor[fl + 1]);
+    float *d_table = grad ? p.acc[fl + 1] : nullptr;
+    for (int strip = 0; strip < p.rank; strip += kStrip) {
+        int64_t f = holder(ends, p.fibres, first), end = 0;
+        float h[4], sum[4] = {0.f, 0.f, 0.f, 0.f}, score = 0.f, weight = 0.f;
+        bool fresh = true;
+        for (int64_t e = first; e <= last; ++e) {
+            if (!fresh && (e == end || e == last)) {
+                score = warp_sum(score);
+                if (lane == 0) {
+                    atomicAdd(p.xs + f, score);
+                    if (strip == 0) atomicAdd(p.weight + f, weight);
+                }
+                if (grad)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = strip + lane + kWarp * q;
+                        if (r < p.rank) atomicAdd(p.xc + f * p.rank + r, sum[q]);
+                    }
+                score = weight = 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum[q] = 0.f;
+                ++f;
+                fresh = true;
+            }
+            if (e == last) break;
+            if (fresh) {
+                int32_t at[kMaxOrder - 1];
+                path_of(p, f, at);
+                end = __ldg(ends + f + 1);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = strip + lane + kWarp * q;
+                    h[q] = r < p.rank ? row_value<T>(p, at, r) : 0.f;
+                }
+                fresh = false;
+            }
+            const float x = __ldg(p.x + e);
+            const int64_t row = (int64_t)__ldg(p.crd[fl + 1] + e) * p.rank;
+            weight += x;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = strip + lane + kWarp * q;
+                if (r >= p.rank) continue;
+                const float c = value(table, row + r);
+                score = fmaf(x * h[q], c, score);
+                sum[q] = fmaf(x, c, sum[q]);
+                if (d_table) atomicAdd(d_table + row + r, -p.scale * x * h[q]);
+            }
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) loss_prepare(const __grid_constant__ Problem p, bool grad) {
+    after_last_kernel();
+    const int64_t warps = (int64_t)gridDim.x * kWarps, me = (int64_t)blockIdx.x * kWarps + threadIdx.x / kWarp;
+    const int64_t runs = (p.leaves + kRun - 1) / kRun;
+    for (int64_t i = me; i < p.fibres + runs; i += warps) {
+        if (i < p.fibres) {
+            make_row<T>(p, i);
+        } else {
+            const int64_t first = (i - p.fibres) * kRun;
+            walk_leaves<T>(p, first, min(first + (int64_t)kRun, p.leaves), grad);
+        }
+    }
+    start_next_kernel();
+}
+
+// ------------------------------------------------------------------------------------------------
+// the passes on the fp32 pipes: tiles of 64 x 64 scores, 4 x 4 a thread
+// ------------------------------------------------------------------------------------------------
+constexpr int kTile = 64, kDeep = 16, kPad = 4;
+
+struct FlatArgs {
+    const void *own, *other;       // [n][rank]
+    int64_t n_own, n_other;
+    int rank, wide;                // columns of the result a block makes; the blocks of gridDim.y make the next ones
+    const float *base, *pull;      // of the other rows (kColumns)
+    Parts parts;
+};
+
+template <typename A, typename B, int PASS>
+__global__ void __launch_bounds__(kThreads) loss_flat(const __grid_constant__ FlatArgs a) {
+    __shared__ __align__(16) float own[kDeep][kTile + kPad], other[kDeep][kTile + kPad];
+    __shared__ __align__(16) float share[kTile][kTile + kPad], piece[kTile][kTile + kPad];
+    after_last_kernel();
+    const A *Q = static_cast<const A *>(a.own);
+    const B *K = static_cast<const B *>(a.other);
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    const int col0 = blockIdx.y * kTile;                             // first column of the sums this block makes
+    const Split &s = a.parts.split;
+    const int64_t u1 = min((int64_t)(blockIdx.x + 1) * s.each, s.groups * s.tiles);
+    for (int64_t u = (int64_t)blockIdx.x * s.each; u < u1;) {
+        const int64_t g = u / s.tiles, t0 = u - g * s.tiles, t1 = min(s.tiles, t0 + (u1 - u));
+        const int64_t q0 = g * kTile;
+        float sum[4][4] = {}, top[4], total[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i] = -INFINITY, total[i] = 0.f;
+        for (int64_t t = t0; t < t1; ++t) {
+            const int64_t k0 = t * kTile;
+            float sc[4][4] = {};
+            for (int r0 = 0; r0 < a.rank; r0 += kDeep) {
+                __syncthreads();
+                for (int e = threadIdx.x; e < kTile * kDeep; e += kThreads) {
+                    const int row = e / kDeep, r = e % kDeep;
+                    own[r][row] = q0 + row < a.n_own && r0 + r < a.rank ? value(Q, (q0 + row) * a.rank + r0 + r) : 0.f;
+                    other[r][row] = k0 + row < a.n_other && r0 + r < a.rank ? value(K, (k0 + row) * a.rank + r0 + r) : 0.f;
+                }
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < kDeep; ++r) {
+                    const float4 x = *reinterpret_cast<const float4 *>(&own[r][4 * ty]);
+                    const float4 y = *reinterpret_cast<const float4 *>(&other[r][4 * tx]);
+                    const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sc[i][j] = fmaf(xs[i], ys[j], sc[i][j]);
+                }
+            }
+            if (PASS == kColumns) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int64_t k = k0 + 4 * tx + j;
+                    const float base = k < a.n_other ? __ldg(a.base + k) : 0.f, pull = k < a.n_other ? __ldg(a.pull + k) : 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[i][j] = pull == 0.f ? 0.f : pull * exp2f(fmaf(sc[i][j], kLog2e, -base));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float m = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (k0 + 4 * tx + j < a.n_other) m = fmaxf(m, sc[i][j]);
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    // in units of log 2 and whole: rescaling is exact, and so is the base that the pass by columns takes
+                    m = fmaxf(ceilf(m * kLog2e), top[i]);
+                    const float keep = exp2f(top[i] - m);           // 0 at the first tile
+                    float part = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        sc[i][j] = k0 + 4 * tx + j < a.n_other ? exp2f(fmaf(sc[i][j], kLog2e, -m)) : 0.f;
+                        part += sc[i][j];
+                    }
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+                    total[i] = total[i] * keep + part;
+                    top[i] = m;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[i][j] *= keep;
+                }
+            }
+            if (PASS == kSum) continue;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<float4 *>(&share[4 * tx + j][4 * ty]) = make_float4(sc[0][j], sc[1][j], sc[2][j], sc[3][j]);
+            for (int e = threadIdx.x; e < kTile * kTile; e += kThreads) {
+                const int row = e / kTile, r = col0 + e % kTile;
+                piece[row][e % kTile] = k0 + row < a.n_other && r < a.rank ? value(K, (k0 + row) * a.rank + r) : 0.f;
+            }
+            __syncthreads();
+            float now[4][4] = {};                                   // a tile's sum first: sums of many tiles lose less
+#pragma unroll 8
+            for (int k = 0; k < kTile; ++k) {
+                const float4 x = *reinterpret_cast<const float4 *>(&share[k][4 * ty]);
+                const float4 y = *reinterpret_cast<const float4 *>(&piece[k][4 * tx]);
+                const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) now[i][j] = fmaf(xs[i], ys[j], now[i][j]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[i][j] += now[i][j];
+        }
+        const int64_t part = g * s.parts + ((int64_t)blockIdx.x - s.first_block(g));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = part * kTile + 4 * ty + i;
+            if (PASS != kColumns && blockIdx.y == 0 && tx == 0) {
+                a.parts.top[row] = top[i];
+                a.parts.total[row] = total[i];
+            }
+            if (PASS != kSum) *reinterpret_cast<float4 *>(a.parts.sum + row * a.parts.width + col0 + 4 * tx) = make_float4(sum[i][0], sum[i][1], sum[i][2], sum[i][3]);
+        }
+        u += t1 - t0;
+    }
+    start_next_kernel();
+}
+
+// ------------------------------------------------------------------------------------------------
+// joining the parts
+// ------------------------------------------------------------------------------------------------
+
+// One warp a fibre: its loss, and with a gradient dh scattered to the factors above the leaves.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Problem p, const __grid_constant__ Parts parts, bool grad) {
+    after_last_kernel();
+    const int lane = threadIdx.x % kWarp;
+    const int64_t warps = (int64_t)gridDim.x * kWarps;
+    for (int64_t f = (int64_t)blockIdx.x * kWarps + threadIdx.x / kWarp; f < p.fibres; f += warps) {
+        const int64_t g = f / parts.split.rows, row = f - g * parts.split.rows, first = g * parts.split.parts;
+        const int n = parts.split.parts_of(g);
+        float top = -INFINITY, total = 0.f;
+        bool bad = false;
+        for (int s = 0; s < n; ++s) {
+            const float t = parts.top[(first + s) * parts.split.rows + row];
+            top = fmaxf(top, t);
+            bad |= t != t;
+        }
+        for (int s = 0; s < n; ++s) {
+            const int64_t at = (first + s) * parts.split.rows + row;
+            total += parts.total[at] * exp2f(parts.top[at] - top);
+        }
+        const float w = p.weight[f];
+        if (bad) total = NAN;
+        if (lane == 0) {
+            p.out[f] = w * fmaf(top, kLn2, logf(total)) - p.xs[f];
+            if (grad) p.base[f] = top, p.pull[f] = w / total;
+        }
+        if (!grad) continue;
+        int32_t at[kMaxOrder - 1];
+        for (int l = 0; l + 1 < p.order; ++l) at[l] = p.path[l][f];
+        const float share = w / total;
+        for (int r = lane; r < p.rank; r += kWarp) {
+            float sum = 0.f;
+            for (int s = 0; s < n; ++s) {
+                const int64_t part = (first + s) * parts.split.rows + row;
+                sum = fmaf(parts.sum[part * parts.width + r], exp2f(parts.top[part] - top), sum);
+            }
+            const float dh = p.scale * (share * sum - p.xc[f * p.rank + r]);
+            for (int l = 0; l + 1 < p.order; ++l) {
+                if (!p.acc[l]) continue;
+                float d = dh;
+                for (int m = 0; m + 1 < p.order; ++m)
+                    if (m != l) d *= value(static_cast<const T *>(p.factor[m]), (int64_t)at[m] * p.rank + r);
+                atomicAdd(p.acc[l] + (int64_t)at[l] * p.rank + r, d);
+            }
+        }
+    }
+    start_next_kernel();
+}
+
+// The gradient of the leaf mode's factor from its parts, and every gradient in the type that was asked for.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) loss_finish(const __grid_constant__ Problem p, const __grid_constant__ Parts parts) {
+    after_last_kernel();
+    start_next_kernel();
+    const int64_t me = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
+    const int leaf = p.order - 1;
+    if (p.grad[leaf])
+        for (int64_t e = me; e < p.extent[leaf] * p.rank; e += all) {
+            const int64_t k = e / p.rank, r = e - k * p.rank;
+            const int64_t g = k / parts.split.rows, row = k - g * parts.split.rows, first = g * parts.split.parts;
+            const int n = parts.split.parts_of(g);
+            float sum = 0.f;
+            for (int s = 0; s < n; ++s) sum += parts.sum[((first + s) * parts.split.rows + row) * parts.width + r];
+            static_cast<T *>(p.grad[leaf])[e] = T(p.acc[leaf][e] + p.scale * sum);
+        }
+    if constexpr (sizeof(T) < sizeof(float))
+        for (int l = 0; l < leaf; ++l)
+            if (p.grad[l])
+                for (int64_t e = me; e < p.extent[l] * p.rank; e += all) static_cast<T *>(p.grad[l])[e] = T(p.acc[l][e]);
+}
+
+int blocks_for(int64_t items, int per_block) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((items + per_block - 1) / per_block, 148 * 8));
+}
+
+struct Arena {
+    int64_t used = 0;
+    char *base = nullptr;
+    template <typename T>
+    T *take(int64_t n) {
+        T *p = base ? reinterpret_cast<T *>(base + used) : nullptr;
+        used += (n * (int64_t)sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+template <typename T>
+const_status_t run(Problem p, bool grad, cudaStream_t stream) {
+    const int leaf = p.order - 1;
+    const bool table = grad && p.grad[leaf];
+    const Split by_rows = split_units(p.fibres, kTile, p.columns, kTile, 148 * 2);
+    const Split by_columns = split_units(p.columns, kTile, p.fibres, kTile, 148 * 2);
+    const int width = (p.rank + kTile - 1) / kTile * kTile;
+    Parts rows, columns;
+    Arena need;
+    char *base = nullptr;
+    Zero zero{};
+    for (int turn = 0; turn < 2; ++turn) {                             // sizes, then places
+        need.used = 0;
+        need.base = base;
+        for (int l = 0; l < leaf; ++l) p.path[l] = need.take<int32_t>(p.fibres);
+        p.h = need.take<float>(p.fibres * p.rank);
+        p.base = need.take<float>(grad ? p.fibres : 0);
+        p.pull = need.take<float>(grad ? p.fibres : 0);
+        const int64_t cleared = need.used;
+        p.xs = need.take<float>(p.fibres);
+        p.weight = need.take<float>(p.fibres);
+        p.xc = need.take<float>(grad ? p.fibres * p.rank : 0);
+        zero.at[kMaxOrder] = base ? reinterpret_cast<float *>(base + cleared) : nullptr;
+        zero.n[kMaxOrder] = (need.used - cleared) / (int64_t)sizeof(float);
+        for (int l = 0; l <= leaf; ++l) {
+            p.acc[l] = nullptr;
+            if (!grad || !p.grad[l]) continue;
+            p.acc[l] = sizeof(T) == sizeof(float) ? static_cast<float *>(p.grad[l]) : need.take<float>(p.extent[l] * p.rank);
+            zero.at[l] = p.acc[l];
+            zero.n[l] = p.extent[l] * p.rank;
+        }
+        const int64_t nr = by_rows.groups * by_rows.parts * by_rows.rows, nc = table ? by_columns.groups * by_columns.parts * by_columns.rows : 0;
+        rows = Parts{by_rows, need.take<float>(grad ? nr * width : 0), need.take<float>(nr), need.take<float>(nr), width};
+        columns = Parts{by_columns, need.take<float>(nc * width), nullptr, nullptr, width};
+        if (turn == 0 && scratch_alloc((void **)&base, (size_t)need.used, stream) != cudaSuccess) {
+            (void)cudaGetLastError();                                  // the next launch must not find this error
+            return CONST_ERR_CUDA;
+        }
+    }
+    cudaError_t e = cudaSuccess;
+    auto ok = [&](cudaError_t now) { if (e == cudaSuccess) e = now; };
+    int64_t zeros = 0;
+    for (int64_t n : zero.n) zeros += n;
+    CB_LAUNCH("loss_clear", stream, ok(launch_early(loss_clear, blocks_for(zeros, 4 * kThreads), kThreads, 0, stream, zero)));
+    const int64_t runs = (p.leaves + kRun - 1) / kRun;
+    CB_LAUNCH("loss_prepare", stream, ok(launch_early(loss_prepare<T>, blocks_for(p.fibres + runs, kWarps), kThreads, 0, stream, p, grad)));
+    FlatArgs a{p.h, p.factor[leaf], p.fibres, p.columns, p.rank, kTile, nullptr, nullptr, rows};
+    auto grid = [&](const Split &s, bool sums) { return dim3((unsigned)((s.groups * s.tiles + s.each - 1) / s.each), sums ? width / kTile : 1); };
+    if (grad)
+        CB_LAUNCH("loss_flat", stream, ok(launch_early(loss_flat<float, T, kRows>, grid(by_rows, true), kThreads, 0, stream, a)));
+    else
+        CB_LAUNCH("loss_flat", stream, ok(launch_early(loss_flat<float, T, kSum>, grid(by_rows, false), kThreads, 0, stream, a)));
+    CB_LAUNCH("loss_rows", stream, ok(launch_early(loss_rows<T>, blocks_for(p.fibres, kWarps), kThreads, 0, stream, p, rows, grad)));
+    if (table) {
+        FlatArgs b{p.factor[leaf], p.h, p.columns, p.fibres, p.rank, kTile, p.base, p.pull, columns};
+        CB_LAUNCH("loss_flat", stream, ok(launch_early(loss_flat<T, float, kColumns>, grid(by_columns, true), kThreads, 0, stream, b)));
+    }
+    if (grad) {
+        int64_t most = 0;
+        for (int l = 0; l <= leaf; ++l) most = std::max(most, p.extent[l] * p.rank);
+        CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T>, blocks_for(most, kThreads), kThreads, 0, stream, p, columns)));
+    }
+    ok(cudaFreeAsync(base, stream));
+    return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) loss_no_rows(T *at, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) at[i] = T(0.f);
+}
+
+}  // namespace
+
+}  // namespace loss
+
+const_status_t run_softmax_loss(const const_csf *X, const void *const *factors, int rank, const_dtype_t dtype, float scale, float *out,
+                                void *const *grads, cudaStream_t stream) {
+    using namespace loss;
+    Problem p{};
+    p.order = X->order;
+    p.rank = rank;
+    p.fibres = X->n[X->order - 2];
+    p.leaves = X->nnz;
+    p.x = static_cast<const float *>(X->vals);
+    p.scale = scale;
+    p.out = out;
+    bool grad = false;
+    for (int l = 0; l < X->order; ++l) {
+        const int mode = X->mode_order[l];
+        p.pos[l] = X->pos[l];
+        p.crd[l] = X->crd[l];
+        p.nodes[l] = X->n[l];
+        p.extent[l] = X->dims[mode];
+        p.factor[l] = factors[mode];
+        p.grad[l] = grads ? grads[mode] : nullptr;
+        grad |= p.grad[l] != nullptr;
+    }
+    p.columns = p.extent[X->order - 1];
+    if (X->nnz == 0) {                                     // no row: nothing to score, and a gradient of zero
+        for (int l = 0; l < X->order; ++l) {
+            if (!p.grad[l]) continue;
+            const int64_t n = p.extent[l] * rank;
+            if (dtype == CONST_F32)
+                CB_LAUNCH("loss_no_rows", stream, loss_no_rows<float><<<blocks_for(n, kThreads), kThreads, 0, stream>>>(static_cast<float *>(p.grad[l]), n));
+            else
+                CB_LAUNCH("loss_no_rows", stream, loss_no_rows<__nv_bfloat16><<<blocks_for(n, kThreads), kThreads, 0, stream>>>(static_cast<__nv_bfloat16 *>(p.grad[l]), n));
+        }
+        return cudaGetLastError() == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
+    }
+    return dtype == CONST_F32 ? run<float>(p, grad, stream) : run<__nv_bfloat16>(p, grad, stream);
+}
+
+}  // namespace cb

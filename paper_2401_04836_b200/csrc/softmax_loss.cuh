@@ -1,0 +1,78 @@
+// Softmax cross entropy over the leaf mode of a CSF tensor: what its kernels share.
+//
+// Rows are the fibres f of the tensor (nodes of level order - 2), columns the coordinates k of the leaf mode.  With h_f the
+// elementwise product of the factor rows on the fibre's path and c_k the row of the leaf mode's factor,
+//     s_fk = <h_f, c_k>,   lse_f = log sum_k exp s_fk,   loss_f = w_f lse_f - sum_leaves x_fk s_fk,   w_f = sum_leaves x_fk
+//     dc_k = scale (sum_f w_f p_fk h_f - sum_leaves x_fk h_f),   p_fk = exp(s_fk - lse_f)
+//     dh_f = scale (w_f sum_k p_fk c_k - sum_leaves x_fk c_k)
+// No score is stored.  Two passes over the F x V scores make all of it: one by rows (running maximum and sum, sum_k p c beside
+// them) and one by columns, which has lse_f and adds up w p h; each makes its tile of scores anew from two operands that stay on
+// chip.  Both are the same loop: a group of "own" rows against all tiles of "other" rows.
+#pragma once
+#include "common.cuh"
+
+namespace cb {
+namespace loss {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// What one pass of the loop over the scores does with a tile of them.
+enum Pass : int {
+    kSum = 0,        // rows: maximum and sum alone (the loss without a gradient)
+    kRows = 1,       // rows: and sum_k p c
+    kColumns = 2     // columns: sum_f w p h, from the rows' maxima and sums
+};
+
+// The groups x tiles units of a pass, dealt to blocks in runs of `each`; a group whose tiles lie in several runs has a part in
+// each, joined by the kernel after.
+struct Split {
+    int64_t groups, tiles;     // groups of own rows, tiles of other rows
+    int64_t each;              // units a block
+    int parts;                 // upper bound of the parts of a group
+    int rows;                  // own rows of a group
+    __host__ __device__ int64_t first_block(int64_t g) const { return g * tiles / each; }
+    __host__ __device__ int parts_of(int64_t g) const { return (int)(((g + 1) * tiles - 1) / each - first_block(g)) + 1; }
+};
+
+inline Split split_units(int64_t own_rows, int rows, int64_t other_rows, int tile, int blocks) {
+    Split s;
+    s.rows = rows;
+    s.groups = (own_rows + rows - 1) / rows;
+    s.tiles = (other_rows + tile - 1) / tile;
+    const int64_t units = s.groups * s.tiles;
+    s.each = (units + blocks - 1) / blocks;
+    if (s.each < 1) s.each = 1;
+    s.parts = (int)((s.tiles + s.each - 1) / s.each) + 1;
+    return s;
+}
+
+// Partial results of a pass: `width` values a row, and for a pass by rows its maximum (in units of log 2) and sum.
+struct Parts {
+    Split split;
+    float *sum;                // [groups * parts][rows][width]
+    float *top, *total;        // [groups * parts][rows]
+    int width;
+};
+
+struct Problem {
+    int order, rank;
+    int64_t fibres, columns, leaves;
+    const int32_t *pos[kMaxOrder], *crd[kMaxOrder];    // of the CSF tensor
+    int64_t nodes[kMaxOrder];
+    const float *x;
+    const void *factor[kMaxOrder];                     // by level, row-major [extent][rank]
+    int64_t extent[kMaxOrder];
+    void *grad[kMaxOrder];                             // results (null: not asked for)
+    float *acc[kMaxOrder];                             // where they are added up, in fp32 (the results themselves if those are fp32)
+    float scale;
+    float *out;                                        // [fibres] losses
+    // scratch
+    int32_t *path[kMaxOrder - 1];                      // [fibres] coordinate of a fibre at every level above the leaves
+    float *h;                                          // [fibres][rank]
+    float *xc;                                         // [fibres][rank] sum_leaves x c (gradient only)
+    float *xs, *weight;                                // [fibres] sum_leaves x s, sum_leaves x
+    float *base, *pull;                                // [fibres] w_f p_fk = pull_f 2^(s_fk / ln 2 - base_f)
+};
+
+}  // namespace loss
+}  // namespace cb

@@ -1,0 +1,146 @@
+"""const_clip_gradients against sums in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2401_04836_b200 as cb
+
+pytestmark = pytest.mark.gpu
+
+# relative: the norm is rounded once from 64 bits, half a step (fp32: sums of up to 8 squares in fp32 are off by 9 halves of a step at
+# most, a square root halves that: 9/2 half steps and the rounding, 6 in all); a value is rounded from a product of two rounded numbers
+HALF = {torch.float32: 2.0 ** -24, torch.float64: 2.0 ** -53, torch.bfloat16: 2.0 ** -8}
+
+
+def make(sizes, dtype, seed=0, size=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return [(torch.randn(n, device="cuda", generator=g, dtype=torch.float64) * size * 10.0 ** (i % 3 - 1)).to(dtype) for i, n in enumerate(sizes)]
+
+
+def clip(grads, max_norm, out=None, **kw):
+    norm = torch.full((1,), float("nan"), device="cuda", dtype=torch.float64 if grads and grads[0].dtype == torch.float64 else torch.float32)
+    cb.const_clip_gradients(grads, max_norm, norm, out=out, **kw)
+    return norm
+
+
+def check(grads, got, norm, max_norm):
+    dtype = grads[0].dtype
+    exact = float(torch.stack([g.double().square().sum() for g in grads]).sum().sqrt())
+    half = 6 * (2.0 ** -53 if dtype == torch.float64 else 2.0 ** -24) + (1e-14 if dtype == torch.float64 else 0.0)   # 64-bit sums on both sides
+    assert abs(float(norm) - exact) <= half * exact
+    factor = min(1.0, max_norm / exact) if exact else 1.0
+    for g, o in zip(grads, got):
+        want = g.double() * factor
+        bound = (HALF[dtype] + 2 * half) * want.abs() + 2.0 ** -133 * (dtype != torch.float64)
+        assert ((o.double() - want).abs() <= bound).all()
+        if factor == 1.0:
+            assert torch.equal(g, o)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float64, torch.bfloat16])
+@pytest.mark.parametrize("sizes", [[1], [3], [1600, 1600, 1600], [4096], [4097, 1, 0, 8191], [8192, 8193, 16384], [0, 5], [1_000_003, 17, 300_000],
+                                   list(range(1, 1700))])
+def test_sizes(sizes, dtype):
+    grads = make(sizes, dtype)
+    whole = float(torch.stack([g.double().square().sum() for g in grads]).sum().sqrt())
+    for factor in (0.01, 0.999, 2.0):
+        out = [torch.full_like(g, float("nan")) for g in grads]
+        check(grads, out, clip(grads, factor * whole, out), factor * whole)
+        place = [g.clone() for g in grads]
+        check(grads, place, clip(place, factor * whole), factor * whole)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_any_address(dtype):
+    """Views at odd offsets of one buffer; the values between them stay as they were."""
+    for off_in, off_out in ((1, 1), (0, 3), (5, 0), (2, 6)):
+        flat, to = torch.randn(60_000, device="cuda").to(dtype), torch.full((60_000,), 9.0, device="cuda", dtype=dtype)
+        grads, out = [flat[off_in:20_000], flat[30_000 + off_in:59_001]], [to[off_out:20_000 + off_out - off_in], to[30_000 + off_out:59_001 + off_out - off_in]]
+        norm = clip(grads, 1.0, out)
+        check(grads, out, norm, 1.0)
+        used = torch.zeros(60_000, dtype=torch.bool, device="cuda")
+        used[off_out:20_000 + off_out - off_in] = True
+        used[30_000 + off_out:59_001 + off_out - off_in] = True
+        assert (to[~used] == 9.0).all()
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-18, 1e18, 1e30])
+def test_squares_beyond_fp32(size):
+    for dtype in (torch.float32, torch.bfloat16):
+        grads = make([5000, 33], dtype, size=size)
+        out = [torch.empty_like(g) for g in grads]
+        check(grads, out, clip(grads, 3.0 * size, out), 3.0 * size)
+
+
+def test_zero_gradients_and_limits():
+    zero = [torch.zeros(1000, device="cuda"), torch.zeros(3, device="cuda")]
+    assert float(clip(zero, 0.0)) == 0.0 and all(torch.count_nonzero(z) == 0 for z in zero)
+    grads = make([1000, 20], torch.float32)
+    same = [g.clone() for g in grads]
+    clip(same, float("inf"))
+    assert all(torch.equal(a, b) for a, b in zip(grads, same))
+    clip(same, 0.0)
+    assert all(torch.count_nonzero(g) == 0 for g in same)
+    assert float(clip([], 1.0)) == 0.0
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float64, torch.bfloat16])
+def test_a_norm_that_is_not_finite_scales_nothing(bad, dtype):
+    grads = make([9000, 70], dtype)
+    grads[1][33] = bad
+    out = [torch.empty_like(g) for g in grads]
+    norm = clip(grads, 0.1, out)
+    assert not torch.isfinite(norm).any() and bool(torch.isnan(norm)) == np.isnan(bad)
+    assert all(torch.equal(torch.nan_to_num(a, 1.5), torch.nan_to_num(b, 1.5)) for a, b in zip(grads, out))
+
+
+def test_the_same_call_gives_the_same_bits():
+    grads = make([1_000_003, 65_537, 12], torch.float32)
+    norms = {float(clip(grads, 1.0, [torch.empty_like(g) for g in grads])) for _ in range(5)}
+    assert len(norms) == 1
+
+
+def test_captured_and_on_another_stream():
+    grads = make([100_003, 65_537, 12], torch.float32)
+    out, norm = [torch.empty_like(g) for g in grads], torch.empty(1, device="cuda")
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        cb.const_clip_gradients(grads, 2.0, norm, out=out)
+    for factor in (1.0, 3.0):
+        for g in grads:
+            g.mul_(factor)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(grads, out, norm, 2.0)
+
+
+def test_refusals():
+    grads, norm = make([100, 20], torch.float32), torch.empty(1, device="cuda")
+    for bad in (dict(max_norm=-1.0), dict(max_norm=float("nan"))):
+        with pytest.raises(cb.ConstError) as e:
+            cb.const_clip_gradients(grads, norm=norm, **bad)
+        assert e.value.status == 1
+    for args in (([grads[0], grads[1].double()], 1.0, norm), ([g.half() for g in grads], 1.0, norm), (grads, 1.0, norm.double()),
+                 ([torch.randn(8, 8, device="cuda").t()], 1.0, norm), ([g.cpu() for g in grads], 1.0, norm)):
+        with pytest.raises(ValueError):
+            cb.const_clip_gradients(*args)
+    with pytest.raises(ValueError):
+        cb.const_clip_gradients(grads, 1.0, norm, out=grads[:1])
+    with pytest.raises(ValueError):
+        cb.const_clip_gradients(grads, 1.0, norm, out=[grads[0], torch.empty(21, device="cuda")])
+
+
+def test_without_scratch():
+    grads, norm = make([100, 20], torch.float32), torch.full((1,), 7.0, device="cuda")
+    before = [g.clone() for g in grads]
+    cb.const_debug_set(3, 1)
+    try:
+        with pytest.raises(cb.ConstError) as e:
+            cb.const_clip_gradients(grads, 0.1, norm)
+        assert e.value.status == 7
+    finally:
+        cb.const_debug_set(3, 0)
+    assert float(norm) == 7.0 and all(torch.equal(a, b) for a, b in zip(grads, before))

@@ -1,0 +1,74 @@
+"""const_softmax_loss and const_clip_gradients refuse bad arguments before any device call, through the C ABI and without a GPU."""
+import ctypes
+
+import numpy as np
+
+import paper_2401_04836_b200 as cb
+from tests.loss_reference import loss_and_gradient
+
+BASE = 0x7F0000001000                                      # never dereferenced
+
+
+def test_softmax_loss_refuses_before_any_device_call():
+    lib = ctypes.CDLL(cb.library_path())
+    lib.const_softmax_loss.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_double, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_void_p]
+    fake = ctypes.create_string_buffer(1024)               # zeroed: no CSF handle
+    factors = (ctypes.c_void_p * 3)(BASE, BASE, BASE)
+    assert lib.const_softmax_loss(None, factors, 8, 0, 1.0, BASE, None, None) == 1
+    assert lib.const_softmax_loss(fake, factors, 8, 0, 1.0, BASE, None, None) == 1
+
+
+def test_clip_gradients_refuses_before_any_device_call():
+    lib = ctypes.CDLL(cb.library_path())
+    lib.const_clip_gradients.argtypes = [ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_double,
+                                         ctypes.c_void_p, ctypes.c_void_p]
+
+    def run(n=1, grads=(BASE,), out=None, sizes=(8,), dtype=0, max_norm=1.0, norm=BASE):
+        g = (ctypes.c_void_p * len(grads))(*grads) if grads is not None else None
+        o = (ctypes.c_void_p * len(out))(*out) if out is not None else None
+        s = (ctypes.c_int64 * len(sizes))(*sizes) if sizes is not None else None
+        return lib.const_clip_gradients(n, g, o, s, dtype, max_norm, norm, None)
+
+    assert run(n=-1) == 1 and run(grads=None) == 1 and run(sizes=None) == 1 and run(norm=None) == 1
+    assert run(sizes=(-1,)) == 1 and run(grads=(None,)) == 1 and run(out=(None,)) == 1
+    assert run(dtype=3) == 1 and run(dtype=-1) == 1
+    assert run(max_norm=-0.5) == 1 and run(max_norm=float("nan")) == 1
+    assert run(grads=(BASE + 2,)) == 1 and run(grads=(BASE + 4,), dtype=1) == 1 and run(grads=(BASE + 1,), dtype=2) == 1
+    assert run(out=(BASE + 2,)) == 1 and run(norm=BASE + 2) == 1 and run(dtype=1, norm=BASE + 4) == 1
+    assert run(sizes=(2 ** 45,)) == 2
+
+
+def test_bf16_is_no_type_of_tensors_or_plans():
+    lib = cb.load_library()
+    out = ctypes.c_void_p()
+    dims, order = (ctypes.c_int64 * 2)(4, 4), (ctypes.c_int * 2)(0, 1)
+    coords = (ctypes.c_void_p * 2)(BASE, BASE)
+    assert lib.const_csf_build(2, dims, 1, coords, BASE, cb.BF16, order, None, ctypes.byref(out)) == 1
+    try:
+        cb.const_plan_create("Y[i,r] = X[i,j] * U[j,r]", ["Y[i,r] = X[i,j] * U[j,r]"], {"X": (0, 1)}, ["ijr"],
+                             {"i": 4, "j": 4, "r": 8}, cb.BF16)
+    except cb.ConstError as e:
+        assert e.status == 1
+    else:
+        raise AssertionError("a plan in bf16")
+
+
+def test_the_reference_against_differences_and_a_closed_form():
+    """The tests' 64-bit definition: a table of equal rows gives log V, and its gradient agrees with differences."""
+    rng = np.random.default_rng(1)
+    coords = [np.array([0, 0, 2, 1]), np.array([1, 3, 0, 2]), np.array([4, 4, 0, 6])]
+    x = np.array([1.0, 0.5, 2.0, 1.0])
+    factors = [rng.standard_normal((3, 5)), rng.standard_normal((4, 5)), np.tile(rng.standard_normal((1, 5)), (7, 1))]
+    (loss, _), _ = loss_and_gradient(coords, x, factors, (0, 1, 2), 1.0)
+    np.testing.assert_allclose(loss, np.array([1.0, 0.5, 1.0, 2.0]) * np.log(7.0), rtol=1e-13)
+    factors[2] = rng.standard_normal((7, 5))
+    _, grads = loss_and_gradient(coords, x, factors, (0, 1, 2), 0.7)
+    for m in range(3):
+        for at in ((0, 0), (2, 3)):
+            ends = []
+            for s in (-1e-5, 1e-5):
+                moved = [f.copy() for f in factors]
+                moved[m][at] += s
+                ends.append(loss_and_gradient(coords, x, moved, (0, 1, 2), 0.7)[0][0].sum() * 0.7)
+            np.testing.assert_allclose(grads[m][0][at], (ends[1] - ends[0]) / 2e-5, rtol=1e-6, atol=1e-9)
