@@ -1,6 +1,7 @@
 // Softmax cross entropy over the leaf mode of a CSF tensor, with its gradient: the steps around the two passes over the
 // scores, the passes on the fp32 pipes, and the host side.  (softmax_loss.cuh has the mathematics.)
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include <algorithm>
 
@@ -68,14 +69,35 @@ __device__ __forceinline__ void path_of(const Problem &p, int64_t f, int32_t *at
     }
 }
 
-// One warp a fibre: its path and its row h.
+__device__ __forceinline__ float larger_finite(float most, float v) {
+    v = fabsf(v);
+    return v < INFINITY ? fmaxf(most, v) : most;
+}
+// The largest of the block's values to a word that started at zero.
+__device__ __forceinline__ void keep_largest(uint32_t *word, float v) {
+    __shared__ uint32_t most;
+    if (threadIdx.x == 0) most = 0;
+    __syncthreads();
+    const uint32_t warp = __reduce_max_sync(0xffffffffu, __float_as_uint(v));     // magnitudes order as their bits do
+    if (threadIdx.x % kWarp == 0 && warp) atomicMax(&most, warp);
+    __syncthreads();
+    if (threadIdx.x == 0 && most) atomicMax(word, most);
+    __syncthreads();
+}
+
+// One warp a fibre: its path and its row h, of which it returns the largest magnitude.
 template <typename T>
-__device__ __forceinline__ void make_row(const Problem &p, int64_t f) {
+__device__ __forceinline__ float make_row(const Problem &p, int64_t f, float most) {
     const int lane = threadIdx.x % kWarp;
     int32_t at[kMaxOrder - 1];
     path_of(p, f, at);
     for (int l = lane; l + 1 < p.order; l += kWarp) p.path[l][f] = at[l];
-    for (int r = lane; r < p.rank; r += kWarp) p.h[f * p.rank + r] = row_value<T>(p, at, r);
+    for (int r = lane; r < p.rank; r += kWarp) {
+        const float h = row_value<T>(p, at, r);
+        p.h[f * p.rank + r] = h;
+        most = larger_finite(most, h);
+    }
+    return most;
 }
 
 // One warp a run of kRun leaves, whatever fibres they lie in: weights, target scores and, with a gradient, the targets' share of
@@ -144,14 +166,62 @@ __global__ void __launch_bounds__(kThreads) loss_prepare(const __grid_constant__
     after_last_kernel();
     const int64_t warps = (int64_t)gridDim.x * kWarps, me = (int64_t)blockIdx.x * kWarps + threadIdx.x / kWarp;
     const int64_t runs = (p.leaves + kRun - 1) / kRun;
+    float most_h = 0.f, most_c = 0.f;
     for (int64_t i = me; i < p.fibres + runs; i += warps) {
         if (i < p.fibres) {
-            make_row<T>(p, i);
+            most_h = make_row<T>(p, i, most_h);
         } else {
             const int64_t first = (i - p.fibres) * kRun;
             walk_leaves<T>(p, first, min(first + (int64_t)kRun, p.leaves), grad);
         }
     }
+    if (p.tensor) {
+        const T *table = static_cast<const T *>(p.factor[p.order - 1]);
+        const int64_t n = p.columns * p.rank, all = (int64_t)gridDim.x * kThreads;
+        for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += all) most_c = larger_finite(most_c, value(table, i));
+        keep_largest(p.words + kMaxH, most_h);
+        keep_largest(p.words + kMaxC, most_c);
+    }
+    start_next_kernel();
+}
+
+// The images of rows and table (softmax_loss.cuh), 16 bytes of each term a thread; and the largest weight of a row.
+template <typename T>
+__device__ __forceinline__ void write_image(const Image &image, const T *from, int64_t rows, int rank, int e, int64_t me, int64_t all) {
+    const int groups = image_columns(rank) / 8;
+    const float up = exp2f((float)e);
+    for (int64_t i = me; i < image_rows(rows) * groups; i += all) {
+        const int64_t v = i / (8 * groups) * 8 + i % 8;
+        const int r0 = (int)(i / 8 % groups) * 8;
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float x[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int r = r0 + 2 * j + k;
+                x[k] = v < rows && r < rank ? value(from, v * rank + r) * up : 0.f;
+            }
+            const __half2 h = __floats2half2_rn(x[0], x[1]);
+            const float2 back = __half22float2(h);
+            const __half2 l = __floats2half2_rn(x[0] - back.x, x[1] - back.y);
+            hi[j] = *reinterpret_cast<const uint32_t *>(&h);
+            lo[j] = *reinterpret_cast<const uint32_t *>(&l);
+        }
+        reinterpret_cast<uint4 *>(image.hi)[i] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if (image.lo) reinterpret_cast<uint4 *>(image.lo)[i] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) loss_images(const __grid_constant__ Problem p, Image rows, Image table) {
+    after_last_kernel();
+    const int64_t me = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
+    write_image(rows, p.h, p.fibres, p.rank, image_exponent(p.words[kMaxH]), me, all);
+    write_image(table, static_cast<const T *>(p.factor[p.order - 1]), p.columns, p.rank, image_exponent(p.words[kMaxC]), me, all);
+    float most = 0.f;
+    for (int64_t f = me; f < p.fibres; f += all) most = larger_finite(most, p.weight[f]);
+    keep_largest(p.words + kMaxWeight, most);
     start_next_kernel();
 }
 
@@ -163,8 +233,8 @@ constexpr int kTile = 64, kDeep = 16, kPad = 4;
 struct FlatArgs {
     const void *own, *other;       // [n][rank]
     int64_t n_own, n_other;
-    int rank, wide;                // columns of the result a block makes; the blocks of gridDim.y make the next ones
-    const float *base, *pull;      // of the other rows (kColumns)
+    int rank;                      // blockIdx.y: which 64 columns of the sums a block makes
+    const float *base, *pull;      // of the other rows (kByColumns)
     Parts parts;
 };
 
@@ -207,7 +277,7 @@ __global__ void __launch_bounds__(kThreads) loss_flat(const __grid_constant__ Fl
                         for (int j = 0; j < 4; ++j) sc[i][j] = fmaf(xs[i], ys[j], sc[i][j]);
                 }
             }
-            if (PASS == kColumns) {
+            if (PASS == kByColumns) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int64_t k = k0 + 4 * tx + j;
@@ -241,7 +311,7 @@ __global__ void __launch_bounds__(kThreads) loss_flat(const __grid_constant__ Fl
                     for (int j = 0; j < 4; ++j) sum[i][j] *= keep;
                 }
             }
-            if (PASS == kSum) continue;
+            if (PASS == kLossAlone) continue;
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -271,11 +341,11 @@ __global__ void __launch_bounds__(kThreads) loss_flat(const __grid_constant__ Fl
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t row = part * kTile + 4 * ty + i;
-            if (PASS != kColumns && blockIdx.y == 0 && tx == 0) {
+            if (PASS != kByColumns && blockIdx.y == 0 && tx == 0) {
                 a.parts.top[row] = top[i];
                 a.parts.total[row] = total[i];
             }
-            if (PASS != kSum) *reinterpret_cast<float4 *>(a.parts.sum + row * a.parts.width + col0 + 4 * tx) = make_float4(sum[i][0], sum[i][1], sum[i][2], sum[i][3]);
+            if (PASS != kLossAlone) *reinterpret_cast<float4 *>(a.parts.sum + row * a.parts.width + col0 + 4 * tx) = make_float4(sum[i][0], sum[i][1], sum[i][2], sum[i][3]);
         }
         u += t1 - t0;
     }
@@ -292,11 +362,13 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
     after_last_kernel();
     const int lane = threadIdx.x % kWarp;
     const int64_t warps = (int64_t)gridDim.x * kWarps;
+    const bool gave_up = p.words[kGaveUp] != 0;
+    const float pull = p.tensor ? exp2f((float)image_exponent(p.words[kMaxWeight])) : 1.f;
     for (int64_t f = (int64_t)blockIdx.x * kWarps + threadIdx.x / kWarp; f < p.fibres; f += warps) {
         const int64_t g = f / parts.split.rows, row = f - g * parts.split.rows, first = g * parts.split.parts;
         const int n = parts.split.parts_of(g);
         float top = -INFINITY, total = 0.f;
-        bool bad = false;
+        bool bad = gave_up;
         for (int s = 0; s < n; ++s) {
             const float t = parts.top[(first + s) * parts.split.rows + row];
             top = fmaxf(top, t);
@@ -310,7 +382,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
         if (bad) total = NAN;
         if (lane == 0) {
             p.out[f] = w * fmaf(top, kLn2, logf(total)) - p.xs[f];
-            if (grad) p.base[f] = top, p.pull[f] = w / total;
+            if (grad) p.base[f] = top, p.pull[f] = w / total * pull;
         }
         if (!grad) continue;
         int32_t at[kMaxOrder - 1];
@@ -342,6 +414,7 @@ __global__ void __launch_bounds__(kThreads) loss_finish(const __grid_constant__ 
     start_next_kernel();
     const int64_t me = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
     const int leaf = p.order - 1;
+    const float gave_up = p.words[kGaveUp] ? NAN : 0.f;
     if (p.grad[leaf])
         for (int64_t e = me; e < p.extent[leaf] * p.rank; e += all) {
             const int64_t k = e / p.rank, r = e - k * p.rank;
@@ -349,12 +422,12 @@ __global__ void __launch_bounds__(kThreads) loss_finish(const __grid_constant__ 
             const int n = parts.split.parts_of(g);
             float sum = 0.f;
             for (int s = 0; s < n; ++s) sum += parts.sum[((first + s) * parts.split.rows + row) * parts.width + r];
-            static_cast<T *>(p.grad[leaf])[e] = T(p.acc[leaf][e] + p.scale * sum);
+            static_cast<T *>(p.grad[leaf])[e] = T(p.acc[leaf][e] + p.scale * sum + gave_up);
         }
-    if constexpr (sizeof(T) < sizeof(float))
+    if (sizeof(T) < sizeof(float) || gave_up != 0.f)
         for (int l = 0; l < leaf; ++l)
             if (p.grad[l])
-                for (int64_t e = me; e < p.extent[l] * p.rank; e += all) static_cast<T *>(p.grad[l])[e] = T(p.acc[l][e]);
+                for (int64_t e = me; e < p.extent[l] * p.rank; e += all) static_cast<T *>(p.grad[l])[e] = T(p.acc[l][e] + gave_up);
 }
 
 int blocks_for(int64_t items, int per_block) {
@@ -374,12 +447,17 @@ struct Arena {
 
 template <typename T>
 const_status_t run(Problem p, bool grad, cudaStream_t stream) {
+    constexpr bool kWide = sizeof(T) == sizeof(float);
     const int leaf = p.order - 1;
     const bool table = grad && p.grad[leaf];
-    const Split by_rows = split_units(p.fibres, kTile, p.columns, kTile, 148 * 2);
-    const Split by_columns = split_units(p.columns, kTile, p.fibres, kTile, 148 * 2);
-    const int width = (p.rank + kTile - 1) / kTile * kTile;
-    Parts rows, columns;
+    p.tensor = p.rank <= kTensorRank;
+    const int own = p.tensor ? kTensorRows : kTile, other = p.tensor ? tensor_tile(p.rank, kWide) : kTile, blocks = p.tensor ? 148 : 148 * 2;
+    const Split by_rows = split_units(p.fibres, own, p.columns, other, blocks);
+    const Split by_columns = split_units(p.columns, own, p.fibres, other, blocks);
+    const int columns = image_columns(p.rank), width = p.tensor ? columns : (p.rank + kTile - 1) / kTile * kTile;
+    const int64_t padded = image_rows(p.fibres);
+    Parts rows, cols;
+    Image image_h{}, image_c{};
     Arena need;
     char *base = nullptr;
     Zero zero{};
@@ -388,24 +466,31 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
         need.base = base;
         for (int l = 0; l < leaf; ++l) p.path[l] = need.take<int32_t>(p.fibres);
         p.h = need.take<float>(p.fibres * p.rank);
-        p.base = need.take<float>(grad ? p.fibres : 0);
-        p.pull = need.take<float>(grad ? p.fibres : 0);
         const int64_t cleared = need.used;
+        p.words = need.take<uint32_t>(kWords);
         p.xs = need.take<float>(p.fibres);
         p.weight = need.take<float>(p.fibres);
+        p.base = need.take<float>(grad ? padded : 0);
+        p.pull = need.take<float>(grad ? padded : 0);
         p.xc = need.take<float>(grad ? p.fibres * p.rank : 0);
         zero.at[kMaxOrder] = base ? reinterpret_cast<float *>(base + cleared) : nullptr;
         zero.n[kMaxOrder] = (need.used - cleared) / (int64_t)sizeof(float);
         for (int l = 0; l <= leaf; ++l) {
             p.acc[l] = nullptr;
             if (!grad || !p.grad[l]) continue;
-            p.acc[l] = sizeof(T) == sizeof(float) ? static_cast<float *>(p.grad[l]) : need.take<float>(p.extent[l] * p.rank);
+            p.acc[l] = kWide ? static_cast<float *>(p.grad[l]) : need.take<float>(p.extent[l] * p.rank);
             zero.at[l] = p.acc[l];
             zero.n[l] = p.extent[l] * p.rank;
         }
+        if (p.tensor) {
+            image_h.hi = need.take<uint16_t>(padded * columns);
+            image_h.lo = need.take<uint16_t>(padded * columns);
+            image_c.hi = need.take<uint16_t>(image_rows(p.columns) * columns);
+            if (kWide) image_c.lo = need.take<uint16_t>(image_rows(p.columns) * columns);     // bf16 has 8 bits: fp16 holds them
+        }
         const int64_t nr = by_rows.groups * by_rows.parts * by_rows.rows, nc = table ? by_columns.groups * by_columns.parts * by_columns.rows : 0;
         rows = Parts{by_rows, need.take<float>(grad ? nr * width : 0), need.take<float>(nr), need.take<float>(nr), width};
-        columns = Parts{by_columns, need.take<float>(nc * width), nullptr, nullptr, width};
+        cols = Parts{by_columns, need.take<float>(nc * width), nullptr, nullptr, width};
         if (turn == 0 && scratch_alloc((void **)&base, (size_t)need.used, stream) != cudaSuccess) {
             (void)cudaGetLastError();                                  // the next launch must not find this error
             return CONST_ERR_CUDA;
@@ -416,23 +501,37 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     int64_t zeros = 0;
     for (int64_t n : zero.n) zeros += n;
     CB_LAUNCH("loss_clear", stream, ok(launch_early(loss_clear, blocks_for(zeros, 4 * kThreads), kThreads, 0, stream, zero)));
-    const int64_t runs = (p.leaves + kRun - 1) / kRun;
-    CB_LAUNCH("loss_prepare", stream, ok(launch_early(loss_prepare<T>, blocks_for(p.fibres + runs, kWarps), kThreads, 0, stream, p, grad)));
-    FlatArgs a{p.h, p.factor[leaf], p.fibres, p.columns, p.rank, kTile, nullptr, nullptr, rows};
-    auto grid = [&](const Split &s, bool sums) { return dim3((unsigned)((s.groups * s.tiles + s.each - 1) / s.each), sums ? width / kTile : 1); };
-    if (grad)
-        CB_LAUNCH("loss_flat", stream, ok(launch_early(loss_flat<float, T, kRows>, grid(by_rows, true), kThreads, 0, stream, a)));
-    else
-        CB_LAUNCH("loss_flat", stream, ok(launch_early(loss_flat<float, T, kSum>, grid(by_rows, false), kThreads, 0, stream, a)));
+    const int64_t runs = (p.leaves + kRun - 1) / kRun, values = p.tensor ? p.columns * p.rank / 32 : 0;
+    CB_LAUNCH("loss_prepare", stream, ok(launch_early(loss_prepare<T>, blocks_for(std::max(p.fibres + runs, values / kWarp), kWarps), kThreads, 0, stream, p, grad)));
+    if (p.tensor)
+        CB_LAUNCH("loss_images", stream, ok(launch_early(loss_images<T>, blocks_for((padded + image_rows(p.columns)) * (columns / 8), kThreads), kThreads, 0, stream, p, image_h, image_c)));
+    auto pass = [&](int which, const Parts &to) {
+        const Split &s = to.split;
+        const int runs_of_units = (int)((s.groups * s.tiles + s.each - 1) / s.each);
+        const bool turned = which == kByColumns;
+        if (p.tensor) {
+            const DebugKnobs knobs = debug_knobs();
+            const TensorArgs a{turned ? image_c : image_h, turned ? image_h : image_c, turned ? p.columns : p.fibres, turned ? p.fibres : p.columns, columns, 0,
+                               p.base, p.pull, p.words, turned ? kMaxC : kMaxH, turned ? kMaxH : kMaxC, p.words + kGaveUp,
+                               knobs.spin_limit ? knobs.spin_limit : 1 << 20, knobs.withhold, s.groups, s.tiles, s.each, s.parts, to.sum, to.top, to.total, to.width};
+            CB_LAUNCH("loss_tensor", stream, ok(tensor_pass(which, kWide, a, runs_of_units, stream)));
+        } else {
+            const FlatArgs a{turned ? p.factor[leaf] : p.h, turned ? p.h : p.factor[leaf], turned ? p.columns : p.fibres, turned ? p.fibres : p.columns, p.rank,
+                             p.base, p.pull, to};
+            const dim3 grid(runs_of_units, which == kLossAlone ? 1 : width / kTile);
+            CB_LAUNCH("loss_flat", stream,
+                      ok(which == kLossAlone ? launch_early(loss_flat<float, T, kLossAlone>, grid, kThreads, 0, stream, a)
+                         : turned            ? launch_early(loss_flat<T, float, kByColumns>, grid, kThreads, 0, stream, a)
+                                             : launch_early(loss_flat<float, T, kByRows>, grid, kThreads, 0, stream, a)));
+        }
+    };
+    pass(grad ? kByRows : kLossAlone, rows);
     CB_LAUNCH("loss_rows", stream, ok(launch_early(loss_rows<T>, blocks_for(p.fibres, kWarps), kThreads, 0, stream, p, rows, grad)));
-    if (table) {
-        FlatArgs b{p.factor[leaf], p.h, p.columns, p.fibres, p.rank, kTile, p.base, p.pull, columns};
-        CB_LAUNCH("loss_flat", stream, ok(launch_early(loss_flat<T, float, kColumns>, grid(by_columns, true), kThreads, 0, stream, b)));
-    }
+    if (table) pass(kByColumns, cols);
     if (grad) {
         int64_t most = 0;
         for (int l = 0; l <= leaf; ++l) most = std::max(most, p.extent[l] * p.rank);
-        CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T>, blocks_for(most, kThreads), kThreads, 0, stream, p, columns)));
+        CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T>, blocks_for(most, kThreads), kThreads, 0, stream, p, cols)));
     }
     ok(cudaFreeAsync(base, stream));
     return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;

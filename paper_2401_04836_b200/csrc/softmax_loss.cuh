@@ -18,9 +18,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // What one pass of the loop over the scores does with a tile of them.
 enum Pass : int {
-    kSum = 0,        // rows: maximum and sum alone (the loss without a gradient)
-    kRows = 1,       // rows: and sum_k p c
-    kColumns = 2     // columns: sum_f w p h, from the rows' maxima and sums
+    kLossAlone = 0,        // rows: maximum and sum alone (the loss without a gradient)
+    kByRows = 1,       // rows: and sum_k p c
+    kByColumns = 2     // columns: sum_f w p h, from the rows' maxima and sums
 };
 
 // The groups x tiles units of a pass, dealt to blocks in runs of `each`; a group whose tiles lie in several runs has a part in
@@ -54,6 +54,51 @@ struct Parts {
     int width;
 };
 
+// Words of scratch that start at zero.
+enum Word : int {
+    kMaxH = 0, kMaxC = 1, kMaxWeight = 2,       // bits of the largest finite magnitude of rows, table and row weights
+    kGaveUp = 3,                                // a bounded wait ran out: the results become NaN
+    kWords = 4
+};
+
+// The passes on the tensor cores (softmax_tensor.cu) have their operands as fp16 images of h and c times a power of two that
+// brings the largest magnitude to [2^13, 2^14): hi + lo with lo = what hi lost, 22 bits in all and 2^-38 of the largest magnitude at least.
+// Rows are padded with zeros to a multiple of kImageRows, columns to a multiple of 16.  Element (v, r) lies in core matrix
+// (v / 8, r / 8), row v % 8, so 8 rows x 8 columns are 128 bytes in one piece and any run of 8 rows is contiguous: the same
+// bytes are a K-major operand with rows as M or N and an MN-major operand with rows as K.
+constexpr int kImageRows = 128;
+constexpr int kTensorRank = 128;                // the largest rank these passes take
+struct Image {
+    uint16_t *hi, *lo;                          // lo: null where hi is exact
+};
+__host__ __device__ inline int64_t image_rows(int64_t n) { return (n + kImageRows - 1) / kImageRows * kImageRows; }
+__host__ __device__ inline int image_columns(int rank) { return (rank + 15) / 16 * 16; }
+
+#ifdef __CUDACC__
+// The exponent of that power of two.
+__device__ __forceinline__ int image_exponent(uint32_t bits) {
+    if (bits == 0) return 0;
+    const int e = 13 - ilogbf(__uint_as_float(bits));
+    return e > 120 ? 120 : e < -120 ? -120 : e;
+}
+#endif
+
+struct TensorArgs {
+    Image own, other;
+    int64_t n_own, n_other;
+    int columns;                                // image_columns(rank)
+    int stages;
+    const float *base, *pull;                   // of the other rows, padded like their image (kByColumns)
+    const uint32_t *words;
+    int own_word, other_word;
+    uint32_t *gave_up;
+    int polls, withhold;
+    int64_t groups, tiles, each;                // as in Split
+    int parts;
+    float *sum, *top, *total;
+    int width;
+};
+
 struct Problem {
     int order, rank;
     int64_t fibres, columns, leaves;
@@ -71,8 +116,16 @@ struct Problem {
     float *h;                                          // [fibres][rank]
     float *xc;                                         // [fibres][rank] sum_leaves x c (gradient only)
     float *xs, *weight;                                // [fibres] sum_leaves x s, sum_leaves x
+    uint32_t *words;                                   // kWords
+    bool tensor;                                       // the passes run on the tensor cores: pull is scaled as the images are
     float *base, *pull;                                // [fibres] w_f p_fk = pull_f 2^(s_fk / ln 2 - base_f)
 };
+
+// softmax_tensor.cu: rows of a group and of a tile, and one pass.  `wide`: factors in fp32 (three products a product, shares of
+// 22 bits), else in bf16 (shares of 11 bits).
+constexpr int kTensorRows = 256;
+int tensor_tile(int rank, bool wide);
+cudaError_t tensor_pass(int pass, bool wide, const TensorArgs &a, int blocks, cudaStream_t stream);
 
 }  // namespace loss
 }  // namespace cb
