@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
     __shared__ uint32_t tmem_at;
     __shared__ int failed_s;
     volatile int *failed = &failed_s;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t row_bytes = 2u * a.columns;
     const uint32_t own_term = kRows * row_bytes, other_term = TN * row_bytes;
     const uint32_t stage_bytes = KT * other_term + (PASS == kByColumns ? 8u * TN : 0u);
@@ -148,35 +148,41 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
         }
         __syncwarp();
     } else if (warp == kIssuer) {
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t i_scores = idesc_f16(kRows, TN, false), i_sums = idesc_f16(kRows, a.columns, true);
             const uint32_t group_rows = 8 * row_bytes;               // bytes of 8 rows: 8 columns of them are 128 bytes
+            const int deep = a.columns / 16;
             uint32_t n = 0, run = 0, made[kGroups] = {0, 0};
-            auto other = [&](uint32_t i) { return other_at + (i % a.stages) * stage_bytes; };
+            // descriptors of the first 16 columns (scores) or rows (sums); further ones, terms and stages lie a constant apart
+            const uint64_t own_k = smem_desc(own_at, 128, group_rows), other_k = smem_desc(other_at, 128, group_rows);
+            const uint64_t other_mn = smem_desc(other_at, group_rows, 128);
+            const uint32_t q_term = own_term >> 4, k_term = other_term >> 4, k_stage = stage_bytes >> 4, mn_step = (2 * group_rows) >> 4;
             auto scores = [&](int t, uint32_t i, uint32_t to) {
-                const uint32_t q = own_at + t * QT * own_term, k = other(i);
+                if (a.withhold) return;
+                const uint64_t q = own_k + t * QT * q_term, k = other_k + (i % a.stages) * k_stage;
                 bool first = true;
-                auto product = [&](uint32_t qa, uint32_t ka) {
-                    for (int c = 0; c < a.columns / 16; ++c, first = false)
-                        if (!a.withhold)
-                            umma_f16(to, smem_desc(qa + c * 256, 128, group_rows), smem_desc(ka + c * 256, 128, group_rows), i_scores, first ? 0u : 1u);
+                auto product = [&](uint64_t qa, uint64_t ka) {
+#pragma unroll
+                    for (int c = 0; c < RP / 16; ++c, first = false) {
+                        if (c >= deep) break;
+                        umma_f16(to, qa + c * 16, ka + c * 16, i_scores, first ? 0u : 1u);
+                    }
                 };
-                if (QT == 2) product(q + own_term, k);
-                if (KT == 2) product(q, k + other_term);
+                if (QT == 2) product(q + q_term, k);
+                if (KT == 2) product(q, k + k_term);
                 product(q, k);
             };
             auto sums = [&](int t, uint32_t i, uint32_t p, uint32_t to) {
-                const uint32_t k = other(i);
+                if (a.withhold) return;
+                const uint64_t k = other_mn + (i % a.stages) * k_stage;
                 bool first = true;
-                auto product = [&](uint32_t pa, uint32_t ka) {
-#pragma unroll 1
-                    for (int c = 0; c < TN / 16; ++c, first = false)
-                        if (!a.withhold)
-                            umma_f16_ts(to, pa + c * 16, smem_desc(ka + c * 2 * group_rows, group_rows, 128), i_sums, first ? 0u : 1u);
+                auto product = [&](uint32_t pa, uint64_t ka) {
+#pragma unroll
+                    for (int c = 0; c < TN / 16; ++c, first = false) umma_f16_ts(to, pa + c * 16, ka + c * mn_step, i_sums, first ? 0u : 1u);
                 };
                 if (PT == 2) {
                     product(p + 8, k);
-                    product(p, k + other_term);
+                    product(p, k + k_term);
                 }
                 product(p, k);
             };
@@ -429,7 +435,7 @@ cudaError_t launch(TensorArgs a, int blocks, cudaStream_t stream) {
 template <int RP, int TN, bool WIDE>
 cudaError_t by_pass(int pass, const TensorArgs &a, int blocks, cudaStream_t stream) {
     constexpr int PT = WIDE ? 2 : 1;
-    if (pass == kLossAlone) return launch<16, kLossAlone, 2, WIDE ? 2 : 1, PT, TN>(a, blocks, stream);
+    if (pass == kLossAlone) return launch<RP, kLossAlone, 2, WIDE ? 2 : 1, PT, TN>(a, blocks, stream);
     if (pass == kByRows) return launch<RP, kByRows, 2, WIDE ? 2 : 1, PT, TN>(a, blocks, stream);
     return launch<RP, kByColumns, WIDE ? 2 : 1, 2, PT, TN>(a, blocks, stream);
 }
