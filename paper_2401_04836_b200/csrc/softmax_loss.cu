@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kThreads) loss_flat(const __grid_constant__ Fl
                     const int64_t k = k0 + 4 * tx + j;
                     const float base = k < a.n_other ? __ldg(a.base + k) : 0.f, pull = k < a.n_other ? __ldg(a.pull + k) : 0.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[i][j] = pull == 0.f ? 0.f : pull * exp2f(fmaf(sc[i][j], kLog2e, -base));
+                    for (int i = 0; i < 4; ++i) sc[i][j] = pull == 0.f ? 0.f : pull * exp2f(fmaf(sc[i][j], kLog2e, base));
                 }
             } else {
 #pragma unroll
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
         if (bad) total = NAN;
         if (lane == 0) {
             p.out[f] = w * fmaf(top, kLn2, logf(total)) - p.xs[f];
-            if (grad) p.base[f] = top, p.pull[f] = w / total * pull;
+            if (grad) p.base[f] = -top, p.pull[f] = w / total * pull;
         }
         if (!grad) continue;
         int32_t at[kMaxOrder - 1];
@@ -451,7 +451,7 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     const int leaf = p.order - 1;
     const bool table = grad && p.grad[leaf];
     p.tensor = p.rank <= kTensorRank;
-    const int own = p.tensor ? kTensorRows : kTile, other = p.tensor ? tensor_tile(p.rank, kWide) : kTile, blocks = p.tensor ? 148 : 148 * 2;
+    const int own = p.tensor ? tensor_rows(p.rank) : kTile, other = p.tensor ? kTensorTile : kTile, blocks = p.tensor ? 148 : 148 * 2;
     const Split by_rows = split_units(p.fibres, own, p.columns, other, blocks);
     const Split by_columns = split_units(p.columns, own, p.fibres, other, blocks);
     const int columns = image_columns(p.rank), width = p.tensor ? columns : (p.rank + kTile - 1) / kTile * kTile;

@@ -118,13 +118,13 @@ struct Problem {
     float *xs, *weight;                                // [fibres] sum_leaves x s, sum_leaves x
     uint32_t *words;                                   // kWords
     bool tensor;                                       // the passes run on the tensor cores: pull is scaled as the images are
-    float *base, *pull;                                // [fibres] w_f p_fk = pull_f 2^(s_fk / ln 2 - base_f)
+    float *base, *pull;                                // [fibres] w_f p_fk = pull_f 2^(s_fk / ln 2 + base_f)
 };
 
 // softmax_tensor.cu: rows of a group and of a tile, and one pass.  `wide`: factors in fp32 (three products a product, shares of
 // 22 bits), else in bf16 (shares of 11 bits).
-constexpr int kTensorRows = 256;
-int tensor_tile(int rank, bool wide);
+constexpr int kTensorTile = 128;
+int tensor_rows(int rank);                      // own rows of a group
 cudaError_t tensor_pass(int pass, bool wide, const TensorArgs &a, int blocks, cudaStream_t stream);
 
 }  // namespace loss

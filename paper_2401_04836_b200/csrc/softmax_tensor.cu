@@ -23,10 +23,10 @@ namespace {
 
 using namespace umma;
 
-constexpr int kGroups = 2;                       // tiles of own rows
-constexpr int kRows = 128;                       // of a tile: lanes of tensor memory
-constexpr int kLoader = 4 * kGroups, kIssuer = kLoader + 1;
-constexpr int kThreads = 32 * (kIssuer + 1);
+constexpr int kRows = 128;                       // of a tile of own rows: lanes of tensor memory
+constexpr int kMaxTiles = 2;                     // tiles of own rows a block has
+constexpr int kTile = 128;                       // other rows of a tile, half of them to each of two warpgroups
+constexpr int kHalf = kTile / 2;
 constexpr int kMaxStages = 4;
 constexpr int kShift = 4;                        // shares are 2^kShift times too large: small ones stay in fp16's range
 constexpr float kSlack = 11.f;                   // by how much a score may exceed the base (2^(kShift + kSlack) < 65504)
@@ -40,9 +40,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 struct Barriers {
     uint64_t own_full, own_free;                 // the own rows of a run of tiles: there, read for the last time
     uint64_t full[kMaxStages], free[kMaxStages]; // a tile of other rows
-    uint64_t scores[kGroups][2];                 // S of a tile is complete (kLossAlone: two buffers)
-    uint64_t shares[kGroups][2];                 // P of a tile is written (kLossAlone: S has been read)
-    uint64_t sums[kGroups];                      // O of the last tile of a run is complete
+    uint64_t scores[kMaxTiles][2];               // S of a tile is complete (by buffer)
+    uint64_t shares[kMaxTiles][2][2];            // P of a half (by half and buffer) is written, or S read for the last time
+    uint64_t sums[kMaxTiles][2];                 // O of a half is complete
 };
 
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
@@ -72,33 +72,73 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 }
 __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
 
+__host__ __device__ constexpr int tiles_of(int columns) { return columns <= 64 ? 2 : 1; }
+__host__ __device__ constexpr int threads_of(int columns) { return 128 * (2 * tiles_of(columns) + 1); }
+
+// two fp32 values in one register pair: one instruction for both
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float x, float y) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 both(Two v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // RP: room for sums in registers.  QT, KT: terms of own and other rows; PT: terms of a share (its product takes as many of Other).
-template <int RP, int PASS, int QT, int KT, int PT, int TN>
-__global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant__ TensorArgs a) {
+template <int RP, int PASS, int QT, int KT, int PT>
+__global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_constant__ TensorArgs a) {
     constexpr bool kSums = PASS != kLossAlone;
-    constexpr int kBuffers = RP <= 64 ? 2 : 1;                       // of O in tensor memory, which S and O of two tiles share
-    constexpr int kStep = RP <= 64 ? 32 : 16;                        // scores a thread has in registers at once
+    constexpr int kTiles = tiles_of(RP);                             // tiles of own rows
+    constexpr int kBuffers = kTiles == 1 || !kSums ? 2 : 1;          // of S; tensor memory holds kTiles x (S, and O of both halves)
+    constexpr int kSpan = 512 / kTiles;                              // columns of tensor memory a tile has
+    constexpr int kSumsAt = 128 * (kTiles == 1 ? 2 : 1);             // O of half 0 and, kSumsWide further, of half 1
+    constexpr int kSumsWide = kTiles == 1 ? 128 : 64;
+    constexpr int kStep = RP <= 32 ? 32 : 16;                        // scores a thread has in registers at once
+    constexpr int kLoader = 8 * kTiles, kIssuer = kLoader + 1;       // warps; those in front of them make the shares
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ Barriers bars;
+    __shared__ float2 merged[kTiles][kRows];                         // maximum and sum of half 1
     __shared__ uint32_t tmem_at;
-    __shared__ int failed_s;
+    __shared__ int failed_s, gave_up[kTiles];
     volatile int *failed = &failed_s;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t row_bytes = 2u * a.columns;
-    const uint32_t own_term = kRows * row_bytes, other_term = TN * row_bytes;
-    const uint32_t stage_bytes = KT * other_term + (PASS == kByColumns ? 8u * TN : 0u);
-    const uint32_t own_at = smem_u32(smem), other_at = own_at + kGroups * QT * own_term;
+    const uint32_t own_term = kRows * row_bytes, other_term = kTile * row_bytes;
+    const uint32_t stage_bytes = KT * other_term + (PASS == kByColumns ? 8u * kTile : 0u);
+    const uint32_t own_at = smem_u32(smem), other_at = own_at + kTiles * QT * own_term;
 
     if (threadIdx.x == 0) {
         failed_s = 0;
+        for (int t = 0; t < kTiles; ++t) gave_up[t] = 0;
         auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_u32(b)), "r"(n) : "memory"); };
         init(&bars.own_full, 1);
         init(&bars.own_free, 1);
         for (int s = 0; s < kMaxStages; ++s) init(&bars.full[s], 1), init(&bars.free[s], 1);
-        for (int t = 0; t < kGroups; ++t) {
-            for (int b = 0; b < 2; ++b) init(&bars.scores[t][b], 1), init(&bars.shares[t][b], 4);
-            init(&bars.sums[t], 1);
-        }
+        for (int t = 0; t < kMaxTiles; ++t)
+            for (int b = 0; b < 2; ++b) {
+                init(&bars.scores[t][b], 1);
+                init(&bars.sums[t][b], 1);
+                for (int h = 0; h < 2; ++h) init(&bars.shares[t][h][b], 4);
+            }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kIssuer) {
@@ -112,29 +152,32 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
     after_last_kernel();
 
     const int64_t u0 = (int64_t)blockIdx.x * a.each, u1 = min(u0 + a.each, a.groups * a.tiles);
-    if (warp == kLoader) {
-        if (lane == 0) {
+    if (warp >= kLoader) {
+        // of the launch's registers (5 x 96 or 3 x 168, by warpgroups) these warps leave the others 4 x 104 or 2 x 208
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == kLoader && elect_one()) {
             uint32_t n = 0, run = 0, held = 0;                       // tiles, runs and loads of own rows so far
             bool ok = true;
             for (int64_t u = u0; u < u1 && ok; ++run) {
                 const int64_t g = u / a.tiles, t0 = u - g * a.tiles, t1 = min(a.tiles, t0 + (u1 - u));
-                const int live = (g * kGroups + 1) * kRows < a.n_own ? 2 : 1;
+                const int live = (int)min((a.n_own - g * kTiles * kRows + kRows - 1) / kRows, (int64_t)kTiles);
                 if (run && !(ok = wait_for(smem_u32(&bars.own_free), (run - 1) & 1, a.polls, failed))) break;
                 const uint32_t bar = smem_u32(&bars.own_full);
                 expect(bar, live * QT * own_term);
                 ++held;
                 for (int t = 0; t < live; ++t)
                     for (int q = 0; q < QT; ++q)
-                        bulk_load(own_at + (t * QT + q) * own_term, (q ? a.own.lo : a.own.hi) + (g * kGroups + t) * kRows * a.columns, own_term, bar);
+                        bulk_load(own_at + (t * QT + q) * own_term, (q ? a.own.lo : a.own.hi) + (g * kTiles + t) * kRows * a.columns, own_term, bar);
                 for (int64_t t = t0; t < t1; ++t, ++n) {
                     const uint32_t s = n % a.stages;
                     if (n >= (uint32_t)a.stages && !(ok = wait_for(smem_u32(&bars.free[s]), (n / a.stages - 1) & 1, a.polls, failed))) break;
                     const uint32_t full = smem_u32(&bars.full[s]), to = other_at + s * stage_bytes;
                     expect(full, stage_bytes);
-                    for (int q = 0; q < KT; ++q) bulk_load(to + q * other_term, (q ? a.other.lo : a.other.hi) + t * TN * a.columns, other_term, full);
+                    for (int q = 0; q < KT; ++q) bulk_load(to + q * other_term, (q ? a.other.lo : a.other.hi) + t * kTile * a.columns, other_term, full);
                     if (PASS == kByColumns) {
-                        bulk_load(to + KT * other_term, a.base + t * TN, 4 * TN, full);
-                        bulk_load(to + KT * other_term + 4 * TN, a.pull + t * TN, 4 * TN, full);
+                        bulk_load(to + KT * other_term, a.base + t * kTile, 4 * kTile, full);
+                        bulk_load(to + KT * other_term + 4 * kTile, a.pull + t * kTile, 4 * kTile, full);
                     }
                 }
                 u += t1 - t0;
@@ -145,20 +188,19 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                 for (uint32_t i = n > (uint32_t)a.stages ? n - a.stages : 0; i < n; ++i)
                     mbar_wait(smem_u32(&bars.full[i % a.stages]), (i / a.stages) & 1, 1 << 14);
             }
-        }
-        __syncwarp();
-    } else if (warp == kIssuer) {
-        if (elect_one()) {
-            const uint32_t i_scores = idesc_f16(kRows, TN, false), i_sums = idesc_f16(kRows, a.columns, true);
+        } else if (warp == kIssuer && elect_one()) {
+            const uint32_t i_scores = idesc_f16(kRows, kTile, false), i_sums = idesc_f16(kRows, a.columns, true);
             const uint32_t group_rows = 8 * row_bytes;               // bytes of 8 rows: 8 columns of them are 128 bytes
             const int deep = a.columns / 16;
-            uint32_t n = 0, run = 0, made[kGroups] = {0, 0};
             // descriptors of the first 16 columns (scores) or rows (sums); further ones, terms and stages lie a constant apart
             const uint64_t own_k = smem_desc(own_at, 128, group_rows), other_k = smem_desc(other_at, 128, group_rows);
             const uint64_t other_mn = smem_desc(other_at, group_rows, 128);
             const uint32_t q_term = own_term >> 4, k_term = other_term >> 4, k_stage = stage_bytes >> 4, mn_step = (2 * group_rows) >> 4;
-            auto scores = [&](int t, uint32_t i, uint32_t to) {
+            uint32_t n = 0, run = 0, made[kTiles] = {};              // tiles, runs; scores issued of a tile of own rows
+            auto commit = [&](uint64_t *b) { if (!a.withhold) umma_commit(smem_u32(b)); };
+            auto scores = [&](int t, uint32_t i) {
                 if (a.withhold) return;
+                const uint32_t b = made[t] % kBuffers, to = tmem + kSpan * t + 128 * b;
                 const uint64_t q = own_k + t * QT * q_term, k = other_k + (i % a.stages) * k_stage;
                 bool first = true;
                 auto product = [&](uint64_t qa, uint64_t ka) {
@@ -171,67 +213,85 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                 if (QT == 2) product(q + q_term, k);
                 if (KT == 2) product(q, k + k_term);
                 product(q, k);
+                commit(&bars.scores[t][b]);
+                ++made[t];
             };
-            auto sums = [&](int t, uint32_t i, uint32_t p, uint32_t to) {
+            auto sums = [&](int t, int h, uint32_t i, uint32_t b) {
                 if (a.withhold) return;
-                const uint64_t k = other_mn + (i % a.stages) * k_stage;
+                const uint64_t k = other_mn + (i % a.stages) * k_stage + h * (kHalf / 16) * mn_step;
+                const uint32_t to = tmem + kSpan * t + kSumsAt + kSumsWide * h, p = tmem + kSpan * t + 128 * b + kHalf * h;
                 bool first = true;
                 auto product = [&](uint32_t pa, uint64_t ka) {
 #pragma unroll
-                    for (int c = 0; c < TN / 16; ++c, first = false) umma_f16_ts(to, pa + c * 16, ka + c * mn_step, i_sums, first ? 0u : 1u);
+                    for (int c = 0; c < kHalf / 16; ++c, first = false) umma_f16_ts(to, pa + c * 16, ka + c * mn_step, i_sums, first ? 0u : 1u);
                 };
                 if (PT == 2) {
                     product(p + 8, k);
                     product(p, k + k_term);
                 }
                 product(p, k);
+                commit(&bars.sums[t][h]);
             };
-            auto commit = [&](uint64_t *b) { if (!a.withhold) umma_commit(smem_u32(b)); };
             bool ok = true;
+            auto arrived = [&](uint64_t *b, uint32_t parity) {
+                ok = wait_for(smem_u32(b), parity, a.polls, failed);
+                fence_after();
+                return ok;
+            };
             for (int64_t u = u0; u < u1 && ok; ++run) {
                 const int64_t g = u / a.tiles, t0 = u - g * a.tiles;
                 const uint32_t tiles = (uint32_t)(min(a.tiles, t0 + (u1 - u)) - t0);
-                const int live = (g * kGroups + 1) * kRows < a.n_own ? 2 : 1;
-                if (!(ok = wait_for(smem_u32(&bars.own_full), run & 1, a.polls, failed))) break;
-                auto arrived = [&](uint32_t i) {
-                    ok = wait_for(smem_u32(&bars.full[i % a.stages]), (i / a.stages) & 1, a.polls, failed);
-                    fence_after();
-                    return ok;
-                };
-                if (!kSums) {
-                    for (uint32_t i = 0; i < tiles && arrived(n); ++i, ++n) {
-                        for (int t = 0; t < live && ok; ++t) {
+                const int live = (int)min((a.n_own - g * kTiles * kRows + kRows - 1) / kRows, (int64_t)kTiles);
+                if (!arrived(&bars.own_full, run & 1)) break;
+                auto loaded = [&](uint32_t i) { return arrived(&bars.full[i % a.stages], (i / a.stages) & 1); };
+                if constexpr (!kSums) {
+                    for (uint32_t i = 0; i < tiles && loaded(n); ++i, ++n) {
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            if (t >= live) break;
                             const uint32_t b = made[t] & 1, turn = made[t] / 2;
-                            if (turn) ok = wait_for(smem_u32(&bars.shares[t][b]), (turn - 1) & 1, a.polls, failed);
-                            if (!ok) break;
-                            fence_after();
-                            scores(t, n, tmem + 256 * t + 128 * b);
-                            commit(&bars.scores[t][b]);
-                            ++made[t];
+                            if (turn && !(arrived(&bars.shares[t][0][b], (turn - 1) & 1) && arrived(&bars.shares[t][1][b], (turn - 1) & 1))) break;
+                            scores(t, n);
                         }
-                        if (ok) commit(&bars.free[n % a.stages]);
+                        if (!ok) break;
+                        commit(&bars.free[n % a.stages]);
+                    }
+                } else if constexpr (kBuffers == 1) {
+                    if (!loaded(n)) break;
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        if (t < live) scores(t, n);
+                    for (uint32_t i = 0; i < tiles && ok; ++i, ++n) {
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            if (t >= live || !ok) break;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                if (!ok || !arrived(&bars.shares[t][h][0], (made[t] - 1) & 1)) break;
+                                sums(t, h, n, 0);
+                            }
+                            if (!ok) break;
+                            if (t == live - 1) commit(&bars.free[n % a.stages]);
+                            if (i + 1 == tiles) continue;
+                            if (t == 0 && !loaded(n + 1)) break;
+                            scores(t, n + 1);                        // behind the products that read the shares in their place
+                        }
                     }
                 } else {
-                    if (!arrived(n)) break;
-                    for (int t = 0; t < live; ++t) {
-                        scores(t, n, tmem + 256 * t);
-                        commit(&bars.scores[t][0]);
-                    }
+                    if (!loaded(n)) break;
+                    scores(0, n);
                     for (uint32_t i = 0; i < tiles && ok; ++i, ++n) {
-                        for (int t = 0; t < live; ++t) {
-                            if (!(ok = wait_for(smem_u32(&bars.shares[t][0]), made[t] & 1, a.polls, failed))) break;
-                            fence_after();
-                            sums(t, n, tmem + 256 * t, tmem + 256 * t + 128 + (made[t] % kBuffers) * 64);
-                            ++made[t];
-                            if (t == live - 1) commit(&bars.free[n % a.stages]);
-                            if (i + 1 == tiles) {
-                                commit(&bars.sums[t]);
-                            } else {
-                                if (t == 0 && !arrived(n + 1)) break;
-                                scores(t, n + 1, tmem + 256 * t);   // behind the product that reads the shares in its place
-                                commit(&bars.scores[t][0]);
-                            }
+                        const uint32_t b = (made[0] - 1) & 1, turn = (made[0] - 1) / 2;
+                        if (i + 1 < tiles) {
+                            if (!loaded(n + 1)) break;
+                            scores(0, n + 1);                        // behind the products of the tile before, which read that buffer
                         }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (!ok || !arrived(&bars.shares[0][h][b], turn & 1)) break;
+                            sums(0, h, n, b);
+                        }
+                        if (ok) commit(&bars.free[n % a.stages]);
                     }
                 }
                 if (ok) commit(&bars.own_free);
@@ -240,18 +300,26 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
         }
         __syncwarp();
     } else {
-        const int t = warp / 4;
-        const uint32_t mine = tmem + 256 * t + ((uint32_t)(warp % 4) << 21);           // 32 lanes a warp
-        const int row = kRows * t + 32 * (warp % 4) + lane;
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int t = warp / 8, h = warp / 4 % 2;                    // tile of own rows, half of the other rows
+        const uint32_t lanes = tmem + kSpan * t + ((uint32_t)(warp % 4) << 21);        // 32 lanes a warp
+        const uint32_t sums_at = lanes + kSumsAt + kSumsWide * h;
+        const int in_tile = 32 * (warp % 4) + lane;
         // from accumulated scores to units of log 2, and what undoes the scales of the sums
         const int e_own = image_exponent(a.words[a.own_word]), e_other = image_exponent(a.words[a.other_word]);
         const float unit = kLog2e * exp2f((float)-e_own) * exp2f((float)-e_other);
-        uint32_t run = 0, seen = 0, turns = 0;                                         // runs and tiles of this row tile; turns: tiles of all
+        const Two unit2 = two(unit, unit);
+        uint32_t seen = 0, turns = 0;                                // tiles of these rows, tiles of all
         bool ok = true;
+        auto arrived = [&](uint64_t *b, uint32_t parity) {           // for the whole warp or not at all
+            ok = __all_sync(0xffffffffu, wait_for(smem_u32(b), parity, a.polls, failed));
+            fence_after();
+            return ok;
+        };
         for (int64_t u = u0; u < u1 && ok;) {
             const int64_t g = u / a.tiles, t0 = u - g * a.tiles, t1 = min(a.tiles, t0 + (u1 - u));
-            const bool live = (g * kGroups + t) * kRows < a.n_own;
-            if (!live) {
+            if ((g * kTiles + t) * kRows >= a.n_own) {
                 turns += (uint32_t)(t1 - t0);
                 u += t1 - t0;
                 continue;
@@ -260,40 +328,35 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
             float sum[kSums ? RP : 1];
 #pragma unroll
             for (int r = 0; r < (kSums ? RP : 1); ++r) sum[r] = 0.f;
-            auto take = [&](uint32_t buffer, float late) {                             // adds O of a tile, made from shares `late` times too large
+            auto take = [&](float late) {                            // adds O of a tile, made from shares `late` times too large
+                if constexpr (kSums) {
 #pragma unroll
-                for (int c = 0; c < RP / 16; ++c) {
-                    if (16 * c >= a.columns) break;
-                    uint32_t o[16];
-                    tmem_load(mine + 128 + 64 * buffer + 16 * c, o);
-                    tmem_landed(o);
+                    for (int c = 0; c < RP / 16; ++c) {
+                        if (16 * c >= a.columns) break;
+                        uint32_t o[16];
+                        tmem_load(sums_at + 16 * c, o);
+                        tmem_landed(o);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if constexpr (kSums) sum[16 * c + r] = PASS == kByRows ? fmaf(late, __uint_as_float(o[r]), sum[16 * c + r]) : sum[16 * c + r] + __uint_as_float(o[r]);
+                        for (int r = 0; r < 16; ++r)
+                            sum[16 * c + r] = PASS == kByRows ? fmaf(late, __uint_as_float(o[r]), sum[16 * c + r]) : sum[16 * c + r] + __uint_as_float(o[r]);
+                    }
                 }
             };
-            auto arrived = [&](uint64_t *b, uint32_t parity) {                         // for the whole warp or not at all
-                ok = __all_sync(0xffffffffu, wait_for(smem_u32(b), parity, a.polls, failed));
-                fence_after();
-                return ok;
-            };
             for (int64_t tile = t0; tile < t1; ++tile, ++seen, ++turns) {
-                const uint32_t b = kSums ? 0 : seen & 1, s_at = mine + 128 * b;
-                if (!arrived(&bars.scores[t][b], kSums ? seen & 1 : (seen / 2) & 1)) break;
+                const uint32_t b = seen % kBuffers, s_at = lanes + 128 * b + kHalf * h;
+                if (!arrived(&bars.scores[t][b], (seen / kBuffers) & 1)) break;
                 float late = 1.f;
-                // the products of the tile before are complete too: they were issued in front of these scores
-                if (kSums && kBuffers == 1 && tile > t0) take(0, 1.f);
-                const int valid = (int)min(a.n_other - tile * TN, (int64_t)TN);
-                const float *vec = reinterpret_cast<const float *>(smem + (other_at - own_at) + (turns % a.stages) * stage_bytes + KT * other_term);
+                const int valid = (int)min(a.n_other - tile * kTile - kHalf * h, (int64_t)kHalf);
+                const float *vec = reinterpret_cast<const float *>(smem + (other_at - own_at) + (turns % a.stages) * stage_bytes + KT * other_term) + kHalf * h;
                 if (PASS == kByColumns && !arrived(&bars.full[turns % a.stages], (turns / a.stages) & 1)) break;   // base and pull came with the tile
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                Two part[2] = {0, 0};
 #pragma unroll
-                for (int c = 0; c < TN / kStep; ++c) {
+                for (int c = 0; c < kHalf / kStep; ++c) {
                     uint32_t s[kStep];
                     tmem_load(s_at + kStep * c, s);
                     tmem_landed(s);
                     if (PASS != kByColumns) {
-                        if (valid < TN)
+                        if (valid < kHalf)
 #pragma unroll
                             for (int j = 0; j < kStep; ++j)
                                 if (kStep * c + j >= valid) s[j] = 0xff800000u;        // -inf
@@ -308,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                             total *= keep;
                             late *= keep;
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) part[q] *= keep;
+                            for (int q = 0; q < 2; ++q) part[q] = mul2(part[q], two(keep, keep));
                             if (kSums) {
 #pragma unroll
                                 for (int r = 0; r < RP; ++r) sum[r] *= keep;
@@ -343,35 +406,36 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                             }
                         }
                     }
-                    const float base = (PASS == kLossAlone ? 0.f : (float)kShift) - top;
+                    // no score yet (a half without other rows): nothing to subtract, the shares are 2^-inf
+                    const float base = top == -INFINITY ? 0.f : (PASS == kLossAlone ? 0.f : (float)kShift) - top;
+                    const Two base2 = two(base, base);
 #pragma unroll
                     for (int k = 0; k < kStep / 16; ++k) {
                         uint32_t hi[8], lo[8];
 #pragma unroll
                         for (int j = 0; j < 8; j += 2) {
-                            float p[4];
                             const int at = 16 * k + 2 * j;
+                            Two p[2];
+                            ulonglong2 pull;
                             if (PASS == kByColumns) {
-                                const float4 bs = *reinterpret_cast<const float4 *>(vec + kStep * c + at);
-                                const float4 pl = *reinterpret_cast<const float4 *>(vec + TN + kStep * c + at);
-                                p[0] = exp2_fast(fmaf(__uint_as_float(s[at]), unit, -bs.x)) * pl.x;
-                                p[1] = exp2_fast(fmaf(__uint_as_float(s[at + 1]), unit, -bs.y)) * pl.y;
-                                p[2] = exp2_fast(fmaf(__uint_as_float(s[at + 2]), unit, -bs.z)) * pl.z;
-                                p[3] = exp2_fast(fmaf(__uint_as_float(s[at + 3]), unit, -bs.w)) * pl.w;
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    p[i] = exp2_fast(fmaf(__uint_as_float(s[at + i]), unit, base));
-                                    part[i] += p[i];
-                                }
+                                const ulonglong2 bs = *reinterpret_cast<const ulonglong2 *>(vec + kStep * c + at);
+                                pull = *reinterpret_cast<const ulonglong2 *>(vec + kTile + kStep * c + at);
+                                p[0] = bs.x;
+                                p[1] = bs.y;
                             }
-                            if (!kSums) continue;
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                hi[j + i] = pack(p[2 * i], p[2 * i + 1]);
+                                const Two e = fma2(two(__uint_as_float(s[at + 2 * i]), __uint_as_float(s[at + 2 * i + 1])), unit2, PASS == kByColumns ? p[i] : base2);
+                                p[i] = two(exp2_fast(both(e).x), exp2_fast(both(e).y));
+                                if (PASS == kByColumns) p[i] = mul2(p[i], i ? pull.y : pull.x);
+                                else part[i] = add2(part[i], p[i]);
+                                if (!kSums) continue;
+                                const float2 v = both(p[i]);
+                                hi[j + i] = pack(v.x, v.y);
                                 if (PT == 2) {
-                                    const float2 h = unpack(hi[j + i]);
-                                    lo[j + i] = pack(p[2 * i] - h.x, p[2 * i + 1] - h.y);
+                                    const float2 f = unpack(hi[j + i]);
+                                    const float2 l = both(fma2(two(f.x, f.y), two(-1.f, -1.f), p[i]));
+                                    lo[j + i] = pack(l.x, l.y);
                                 }
                             }
                         }
@@ -381,32 +445,74 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                         }
                     }
                 }
-                if (kSums) tmem_stored();
-                fence_before();
-                __syncwarp();
-                if (lane == 0) arrive(smem_u32(&bars.shares[t][b]));
-                total += (part[0] + part[1]) + (part[2] + part[3]);
-                if (kSums && kBuffers == 2 && tile > t0) take((seen - 1) & 1, late);
-            }
-            if (ok && kSums && arrived(&bars.sums[t], run++ & 1)) take(kBuffers == 2 ? (seen - 1) & 1 : 0, 1.f);
-            const int64_t part = (g * a.parts + ((int64_t)blockIdx.x - g * a.tiles / a.each)) * (kGroups * kRows) + row;
-            if (ok) {
-                const float shift = PASS == kByRows ? 1.f / (1 << kShift) : 1.f;
                 if (PASS != kByColumns) {
-                    a.top[part] = top;
-                    a.total[part] = total * shift;
+                    const float2 x = both(add2(part[0], part[1]));
+                    total += x.x + x.y;
                 }
                 if (kSums) {
-                    const float undo = exp2f((float)-e_other) * shift;
-                    float undo2 = 1.f;
-                    if (PASS == kByColumns) undo2 = exp2f((float)-image_exponent(a.words[kMaxWeight]));
+                    if (tile > t0) {                                 // O of the tile before, which the next product overwrites
+                        if (!arrived(&bars.sums[t][h], (seen - 1) & 1)) break;
+                        take(late);
+                    }
+                    tmem_stored();
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) arrive(smem_u32(&bars.shares[t][h][b]));
+            }
+            if (kSums && ok && arrived(&bars.sums[t][h], (seen - 1) & 1)) take(1.f);
+            // Half 1 hands its sums to half 0 where O was: nothing writes there before the shares of half 1 in the next run.
+            if (h == 1) {
+                if constexpr (kSums) {
+#pragma unroll
+                    for (int c = 0; c < RP / 8; ++c) {
+                        if (8 * c >= a.columns) break;
+                        uint32_t w[8];
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) w[r] = __float_as_uint(sum[8 * c + r]);
+                        tmem_store(sums_at + 8 * c, w);
+                    }
+                    tmem_stored();
+                }
+                merged[t][in_tile] = make_float2(top, total);
+                fence_before();
+            }
+            if (!ok) *(volatile int *)&gave_up[t] = 1;
+            asm volatile("bar.sync %0, 256;" :: "r"(1 + t) : "memory");
+            ok = *(volatile int *)&gave_up[t] == 0;                  // the same for both halves: both go on or neither
+            if (h == 0) {
+                fence_after();
+                const int64_t part = (g * a.parts + ((int64_t)blockIdx.x - g * a.tiles / a.each)) * (kTiles * kRows) + kRows * t + in_tile;
+                const float2 other = merged[t][in_tile];
+                const float shift = PASS == kByRows ? 1.f / (1 << kShift) : 1.f;
+                float mine = 1.f, theirs = 1.f;
+                if (PASS != kByColumns) {
+                    const float most = fmaxf(top, other.x);
+                    mine = top == -INFINITY ? 0.f : exp2f(top - most);
+                    theirs = other.x == -INFINITY ? 0.f : exp2f(other.x - most);
+                    a.top[part] = most;
+                    a.total[part] = (total * mine + other.y * theirs) * shift;
+                }
+                if constexpr (kSums) {
+                    const float undo = exp2f((float)-e_other) * shift, undo2 = PASS == kByColumns ? exp2f((float)-image_exponent(a.words[kMaxWeight])) : 1.f;
                     float4 *to = reinterpret_cast<float4 *>(a.sum + part * a.width);
 #pragma unroll
-                    for (int c = 0; c < RP / 4; ++c)
-                        if (4 * c < a.columns)
-                            to[c] = make_float4(sum[4 * c] * undo * undo2, sum[4 * c + 1] * undo * undo2, sum[4 * c + 2] * undo * undo2, sum[4 * c + 3] * undo * undo2);
+                    for (int c = 0; c < RP / 16; ++c) {
+                        if (16 * c >= a.columns) break;
+                        uint32_t o[16];
+                        tmem_load(sums_at + kSumsWide + 16 * c, o);
+                        tmem_landed(o);
+                        float x[16];
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) x[r] = fmaf(sum[16 * c + r], mine, __uint_as_float(o[r]) * theirs) * undo * undo2;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) to[4 * c + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                    }
                 }
+                fence_before();
             }
+            asm volatile("bar.sync %0, 256;" :: "r"(1 + t) : "memory");
+            fence_after();
             u += t1 - t0;
         }
     }
@@ -418,40 +524,39 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
     start_next_kernel();
 }
 
-template <int RP, int PASS, int QT, int KT, int PT, int TN>
+template <int RP, int PASS, int QT, int KT, int PT>
 cudaError_t launch(TensorArgs a, int blocks, cudaStream_t stream) {
-    constexpr int kMost = 226 * 1024;                                // of 227 KB: the barriers are apart
-    const int own = kGroups * QT * kRows * 2 * a.columns, stage = KT * TN * 2 * a.columns + (PASS == kByColumns ? 8 * TN : 0);
+    constexpr int kMost = 224 * 1024;                                // of 227 KB: barriers and what halves exchange are apart
+    const int own = tiles_of(RP) * QT * kRows * 2 * a.columns, stage = KT * kTile * 2 * a.columns + (PASS == kByColumns ? 8 * kTile : 0);
     a.stages = std::min<int>(kMaxStages, (kMost - own) / stage);
     const int bytes = own + a.stages * stage;
     static PerDeviceOnce once;
     const cudaError_t e = once_per_device(once, [] {
-        return cudaFuncSetAttribute(loss_tensor<RP, PASS, QT, KT, PT, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        return cudaFuncSetAttribute(loss_tensor<RP, PASS, QT, KT, PT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     });
     if (e != cudaSuccess) return e;
-    return launch_early(loss_tensor<RP, PASS, QT, KT, PT, TN>, dim3(blocks), kThreads, bytes, stream, a);
+    return launch_early(loss_tensor<RP, PASS, QT, KT, PT>, dim3(blocks), threads_of(RP), bytes, stream, a);
 }
 
-template <int RP, int TN, bool WIDE>
+template <int RP, bool WIDE>
 cudaError_t by_pass(int pass, const TensorArgs &a, int blocks, cudaStream_t stream) {
     constexpr int PT = WIDE ? 2 : 1;
-    if (pass == kLossAlone) return launch<RP, kLossAlone, 2, WIDE ? 2 : 1, PT, TN>(a, blocks, stream);
-    if (pass == kByRows) return launch<RP, kByRows, 2, WIDE ? 2 : 1, PT, TN>(a, blocks, stream);
-    return launch<RP, kByColumns, WIDE ? 2 : 1, 2, PT, TN>(a, blocks, stream);
+    if (pass == kLossAlone) return launch<RP, kLossAlone, 2, WIDE ? 2 : 1, PT>(a, blocks, stream);
+    if (pass == kByRows) return launch<RP, kByRows, 2, WIDE ? 2 : 1, PT>(a, blocks, stream);
+    return launch<RP, kByColumns, WIDE ? 2 : 1, 2, PT>(a, blocks, stream);
 }
 
 template <bool WIDE>
 cudaError_t by_rank(int pass, const TensorArgs &a, int blocks, cudaStream_t stream) {
-    if (a.columns <= 16) return by_pass<16, 128, WIDE>(pass, a, blocks, stream);
-    if (a.columns <= 32) return by_pass<32, 128, WIDE>(pass, a, blocks, stream);
-    if (a.columns <= 64) return by_pass<64, 128, WIDE>(pass, a, blocks, stream);
-    return by_pass<128, WIDE ? 64 : 128, WIDE>(pass, a, blocks, stream);
+    if (a.columns <= 16) return by_pass<16, WIDE>(pass, a, blocks, stream);
+    if (a.columns <= 32) return by_pass<32, WIDE>(pass, a, blocks, stream);
+    if (a.columns <= 64) return by_pass<64, WIDE>(pass, a, blocks, stream);
+    return by_pass<128, WIDE>(pass, a, blocks, stream);
 }
 
 }  // namespace
 
-// Tiles of 128 other rows, or of 64 where 256 own rows of two terms leave no room for two of 128.
-int tensor_tile(int rank, bool wide) { return wide && image_columns(rank) > 64 ? 64 : 128; }
+int tensor_rows(int rank) { return kRows * tiles_of(image_columns(rank)); }
 
 cudaError_t tensor_pass(int pass, bool wide, const TensorArgs &a, int blocks, cudaStream_t stream) {
     return wide ? by_rank<true>(pass, a, blocks, stream) : by_rank<false>(pass, a, blocks, stream);
