@@ -40,9 +40,17 @@ __device__ __forceinline__ float exp2_fast(float x) {
 struct Barriers {
     uint64_t own_full, own_free;                 // the own rows of a run of tiles: there, read for the last time
     uint64_t full[kMaxStages], free[kMaxStages]; // a tile of other rows
-    uint64_t scores[kMaxTiles][2];               // S of a tile is complete (by buffer)
-    uint64_t shares[kMaxTiles][2][2];            // P of a half (by half and buffer) is written, or S read for the last time
-    uint64_t sums[kMaxTiles][2];                 // O of a half is complete
+    uint64_t scores[kMaxTiles][2];               // S of a tile is complete, and every product issued before it (by buffer)
+    uint64_t shares[kMaxTiles][2];               // P of a tile is written, or S read for the last time (by buffer)
+    uint64_t sums[kMaxTiles];                    // O of a tile is complete, where no S issued later says so
+};
+
+// A place in the ring of stages and the parity of its turn.
+struct Place {
+    uint32_t at = 0, turn = 0;
+    __device__ __forceinline__ void next(uint32_t stages) {
+        if (++at == stages) at = 0, turn ^= 1;
+    }
 };
 
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
@@ -58,6 +66,7 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 
 // A wait that gives up after `polls` polls, or soon after another thread of the block has given up.
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int polls, volatile int *failed) {
+    if (mbar_wait(bar, parity, 1)) return true;
     for (int n = 0; n < polls; n += 64) {
         if (mbar_wait(bar, parity, 64)) return true;
         if (*failed) return false;
@@ -136,9 +145,9 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
         for (int t = 0; t < kMaxTiles; ++t)
             for (int b = 0; b < 2; ++b) {
                 init(&bars.scores[t][b], 1);
-                init(&bars.sums[t][b], 1);
-                for (int h = 0; h < 2; ++h) init(&bars.shares[t][h][b], 4);
+                init(&bars.shares[t][b], 8);
             }
+        for (int t = 0; t < kMaxTiles; ++t) init(&bars.sums[t], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kIssuer) {
@@ -157,38 +166,43 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
         if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == kLoader && elect_one()) {
-            uint32_t n = 0, run = 0, held = 0;                       // tiles, runs and loads of own rows so far
+            Place place;
+            uint32_t run = 0, loads = 0;                             // runs begun; tiles loaded, up to the number of stages
             bool ok = true;
-            for (int64_t u = u0; u < u1 && ok; ++run) {
+            for (int64_t u = u0; u < u1 && ok;) {
                 const int64_t g = u / a.tiles, t0 = u - g * a.tiles, t1 = min(a.tiles, t0 + (u1 - u));
                 const int live = (int)min((a.n_own - g * kTiles * kRows + kRows - 1) / kRows, (int64_t)kTiles);
-                if (run && !(ok = wait_for(smem_u32(&bars.own_free), (run - 1) & 1, a.polls, failed))) break;
+                if (!(ok = wait_for(smem_u32(&bars.own_free), (run & 1) ^ 1, a.polls, failed))) break;
                 const uint32_t bar = smem_u32(&bars.own_full);
                 expect(bar, live * QT * own_term);
-                ++held;
+                ++run;
                 for (int t = 0; t < live; ++t)
                     for (int q = 0; q < QT; ++q)
                         bulk_load(own_at + (t * QT + q) * own_term, (q ? a.own.lo : a.own.hi) + (g * kTiles + t) * kRows * a.columns, own_term, bar);
-                for (int64_t t = t0; t < t1; ++t, ++n) {
-                    const uint32_t s = n % a.stages;
-                    if (n >= (uint32_t)a.stages && !(ok = wait_for(smem_u32(&bars.free[s]), (n / a.stages - 1) & 1, a.polls, failed))) break;
-                    const uint32_t full = smem_u32(&bars.full[s]), to = other_at + s * stage_bytes;
+                for (int64_t t = t0; t < t1; ++t) {
+                    if (!(ok = wait_for(smem_u32(&bars.free[place.at]), place.turn ^ 1, a.polls, failed))) break;
+                    const uint32_t full = smem_u32(&bars.full[place.at]), to = other_at + place.at * stage_bytes;
                     expect(full, stage_bytes);
                     for (int q = 0; q < KT; ++q) bulk_load(to + q * other_term, (q ? a.other.lo : a.other.hi) + t * kTile * a.columns, other_term, full);
                     if (PASS == kByColumns) {
                         bulk_load(to + KT * other_term, a.base + t * kTile, 4 * kTile, full);
                         bulk_load(to + KT * other_term + 4 * kTile, a.pull + t * kTile, 4 * kTile, full);
                     }
+                    place.next(a.stages);
+                    loads = min(loads + 1, (uint32_t)a.stages);
                 }
                 u += t1 - t0;
             }
             // nothing of this block is under way when it ends, whatever the others did
             if (!ok) {
-                if (held) mbar_wait(smem_u32(&bars.own_full), (held - 1) & 1, 1 << 14);
-                for (uint32_t i = n > (uint32_t)a.stages ? n - a.stages : 0; i < n; ++i)
-                    mbar_wait(smem_u32(&bars.full[i % a.stages]), (i / a.stages) & 1, 1 << 14);
+                if (run) mbar_wait(smem_u32(&bars.own_full), (run & 1) ^ 1, 1 << 14);
+                for (uint32_t i = 0; i < loads; ++i) {               // the last ones, backwards
+                    if (place.at == 0) place.at = a.stages, place.turn ^= 1;
+                    --place.at;
+                    mbar_wait(smem_u32(&bars.full[place.at]), place.turn, 1 << 14);
+                }
             }
-        } else if (warp == kIssuer && elect_one()) {
+        } else if (warp == kIssuer) {                                // the whole warp: its operands stay in uniform registers
             const uint32_t i_scores = idesc_f16(kRows, kTile, false), i_sums = idesc_f16(kRows, a.columns, true);
             const uint32_t group_rows = 8 * row_bytes;               // bytes of 8 rows: 8 columns of them are 128 bytes
             const int deep = a.columns / 16;
@@ -196,12 +210,13 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
             const uint64_t own_k = smem_desc(own_at, 128, group_rows), other_k = smem_desc(other_at, 128, group_rows);
             const uint64_t other_mn = smem_desc(other_at, group_rows, 128);
             const uint32_t q_term = own_term >> 4, k_term = other_term >> 4, k_stage = stage_bytes >> 4, mn_step = (2 * group_rows) >> 4;
-            uint32_t n = 0, run = 0, made[kTiles] = {};              // tiles, runs; scores issued of a tile of own rows
-            auto commit = [&](uint64_t *b) { if (!a.withhold) umma_commit(smem_u32(b)); };
-            auto scores = [&](int t, uint32_t i) {
-                if (a.withhold) return;
-                const uint32_t b = made[t] % kBuffers, to = tmem + kSpan * t + 128 * b;
-                const uint64_t q = own_k + t * QT * q_term, k = other_k + (i % a.stages) * k_stage;
+            uint32_t run = 0, made = 0;                              // runs; tiles whose scores were issued in all runs before
+            uint32_t made_t[kTiles] = {};                            // the same of each tile of own rows
+            Place place;
+            auto commit = [&](uint64_t *b) { if (!a.withhold && elect_one()) umma_commit(smem_u32(b)); };
+            auto scores = [&](int t, uint32_t stage, uint32_t b) {
+                const uint32_t to = tmem + kSpan * t + 128 * b;
+                const uint64_t q = own_k + t * QT * q_term, k = other_k + stage * k_stage;
                 bool first = true;
                 auto product = [&](uint64_t qa, uint64_t ka) {
 #pragma unroll
@@ -210,88 +225,95 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
                         umma_f16(to, qa + c * 16, ka + c * 16, i_scores, first ? 0u : 1u);
                     }
                 };
-                if (QT == 2) product(q + q_term, k);
-                if (KT == 2) product(q, k + k_term);
-                product(q, k);
-                commit(&bars.scores[t][b]);
-                ++made[t];
-            };
-            auto sums = [&](int t, int h, uint32_t i, uint32_t b) {
-                if (a.withhold) return;
-                const uint64_t k = other_mn + (i % a.stages) * k_stage + h * (kHalf / 16) * mn_step;
-                const uint32_t to = tmem + kSpan * t + kSumsAt + kSumsWide * h, p = tmem + kSpan * t + 128 * b + kHalf * h;
-                bool first = true;
-                auto product = [&](uint32_t pa, uint64_t ka) {
-#pragma unroll
-                    for (int c = 0; c < kHalf / 16; ++c, first = false) umma_f16_ts(to, pa + c * 16, ka + c * mn_step, i_sums, first ? 0u : 1u);
-                };
-                if (PT == 2) {
-                    product(p + 8, k);
-                    product(p, k + k_term);
+                if (!a.withhold && elect_one()) {
+                    if (QT == 2) product(q + q_term, k);
+                    if (KT == 2) product(q, k + k_term);
+                    product(q, k);
+                    umma_commit(smem_u32(&bars.scores[t][b]));
                 }
-                product(p, k);
-                commit(&bars.sums[t][h]);
+                __syncwarp();
+            };
+            auto sums = [&](int t, uint32_t stage, uint32_t b) {
+                const uint64_t k = other_mn + stage * k_stage;
+                const uint32_t to = tmem + kSpan * t + kSumsAt, p = tmem + kSpan * t + 128 * b;
+                if (!a.withhold && elect_one()) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        bool first = true;
+                        auto product = [&](uint32_t pa, uint64_t ka) {
+#pragma unroll
+                            for (int c = h * kHalf / 16; c < (h + 1) * kHalf / 16; ++c, first = false)
+                                umma_f16_ts(to + kSumsWide * h, pa + c * 16, ka + c * mn_step, i_sums, first ? 0u : 1u);
+                        };
+                        if (PT == 2) {
+                            product(p + 8, k);
+                            product(p, k + k_term);
+                        }
+                        product(p, k);
+                    }
+                }
+                __syncwarp();
             };
             bool ok = true;
             auto arrived = [&](uint64_t *b, uint32_t parity) {
-                ok = wait_for(smem_u32(b), parity, a.polls, failed);
+                ok = __all_sync(0xffffffffu, wait_for(smem_u32(b), parity, a.polls, failed));
                 fence_after();
                 return ok;
             };
+            auto loaded = [&](const Place &w) { return arrived(&bars.full[w.at], w.turn); };
             for (int64_t u = u0; u < u1 && ok; ++run) {
                 const int64_t g = u / a.tiles, t0 = u - g * a.tiles;
                 const uint32_t tiles = (uint32_t)(min(a.tiles, t0 + (u1 - u)) - t0);
                 const int live = (int)min((a.n_own - g * kTiles * kRows + kRows - 1) / kRows, (int64_t)kTiles);
                 if (!arrived(&bars.own_full, run & 1)) break;
-                auto loaded = [&](uint32_t i) { return arrived(&bars.full[i % a.stages], (i / a.stages) & 1); };
                 if constexpr (!kSums) {
-                    for (uint32_t i = 0; i < tiles && loaded(n); ++i, ++n) {
-#pragma unroll
-                        for (int t = 0; t < kTiles; ++t) {
-                            if (t >= live) break;
-                            const uint32_t b = made[t] & 1, turn = made[t] / 2;
-                            if (turn && !(arrived(&bars.shares[t][0][b], (turn - 1) & 1) && arrived(&bars.shares[t][1][b], (turn - 1) & 1))) break;
-                            scores(t, n);
-                        }
-                        if (!ok) break;
-                        commit(&bars.free[n % a.stages]);
-                    }
-                } else if constexpr (kBuffers == 1) {
-                    if (!loaded(n)) break;
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t)
-                        if (t < live) scores(t, n);
-                    for (uint32_t i = 0; i < tiles && ok; ++i, ++n) {
+                    for (uint32_t i = 0; i < tiles && loaded(place); ++i) {
 #pragma unroll
                         for (int t = 0; t < kTiles; ++t) {
                             if (t >= live || !ok) break;
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                if (!ok || !arrived(&bars.shares[t][h][0], (made[t] - 1) & 1)) break;
-                                sums(t, h, n, 0);
-                            }
-                            if (!ok) break;
-                            if (t == live - 1) commit(&bars.free[n % a.stages]);
-                            if (i + 1 == tiles) continue;
-                            if (t == 0 && !loaded(n + 1)) break;
-                            scores(t, n + 1);                        // behind the products that read the shares in their place
+                            const uint32_t b = made_t[t] & 1;
+                            if (!arrived(&bars.shares[t][b], (made_t[t] / 2 & 1) ^ 1)) break;
+                            scores(t, place.at, b);
+                            ++made_t[t];
                         }
+                        if (!ok) break;
+                        commit(&bars.free[place.at]);
+                        place.next(a.stages);
+                    }
+                } else if constexpr (kBuffers == 1) {
+                    if (!loaded(place)) break;
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        if (t < live) scores(t, place.at, 0);
+                    for (uint32_t i = 0; i < tiles && ok; ++i) {
+                        Place after = place;
+                        after.next(a.stages);
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            if (t >= live || !ok) break;
+                            if (!arrived(&bars.shares[t][0], made_t[t]++ & 1)) break;
+                            sums(t, place.at, 0);
+                            if (t == live - 1) commit(&bars.free[place.at]);
+                            if (i + 1 == tiles) commit(&bars.sums[t]);
+                            else if (t > 0 || loaded(after)) scores(t, after.at, 0);   // behind the products that read the shares in their place
+                        }
+                        place = after;
                     }
                 } else {
-                    if (!loaded(n)) break;
-                    scores(0, n);
-                    for (uint32_t i = 0; i < tiles && ok; ++i, ++n) {
-                        const uint32_t b = (made[0] - 1) & 1, turn = (made[0] - 1) / 2;
+                    if (!loaded(place)) break;
+                    scores(0, place.at, made & 1);
+                    for (uint32_t i = 0; i < tiles && ok; ++i, ++made) {
+                        Place after = place;
+                        after.next(a.stages);
                         if (i + 1 < tiles) {
-                            if (!loaded(n + 1)) break;
-                            scores(0, n + 1);                        // behind the products of the tile before, which read that buffer
+                            if (!loaded(after)) break;
+                            scores(0, after.at, (made + 1) & 1);     // behind the products of the tile before, which read that buffer
                         }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if (!ok || !arrived(&bars.shares[0][h][b], turn & 1)) break;
-                            sums(0, h, n, b);
-                        }
-                        if (ok) commit(&bars.free[n % a.stages]);
+                        if (!arrived(&bars.shares[0][made & 1], made / 2 & 1)) break;
+                        sums(0, place.at, made & 1);
+                        commit(&bars.sums[0]);
+                        commit(&bars.free[place.at]);
+                        place = after;
                     }
                 }
                 if (ok) commit(&bars.own_free);
@@ -310,7 +332,8 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
         const int e_own = image_exponent(a.words[a.own_word]), e_other = image_exponent(a.words[a.other_word]);
         const float unit = kLog2e * exp2f((float)-e_own) * exp2f((float)-e_other);
         const Two unit2 = two(unit, unit);
-        uint32_t seen = 0, turns = 0;                                // tiles of these rows, tiles of all
+        uint32_t seen = 0, runs = 0;                                 // tiles and runs of these rows
+        Place place;
         bool ok = true;
         auto arrived = [&](uint64_t *b, uint32_t parity) {           // for the whole warp or not at all
             ok = __all_sync(0xffffffffu, wait_for(smem_u32(b), parity, a.polls, failed));
@@ -320,7 +343,8 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
         for (int64_t u = u0; u < u1 && ok;) {
             const int64_t g = u / a.tiles, t0 = u - g * a.tiles, t1 = min(a.tiles, t0 + (u1 - u));
             if ((g * kTiles + t) * kRows >= a.n_own) {
-                turns += (uint32_t)(t1 - t0);
+                if (PASS == kByColumns)
+                    for (int64_t tile = t0; tile < t1; ++tile) place.next(a.stages);
                 u += t1 - t0;
                 continue;
             }
@@ -330,25 +354,34 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
             for (int r = 0; r < (kSums ? RP : 1); ++r) sum[r] = 0.f;
             auto take = [&](float late) {                            // adds O of a tile, made from shares `late` times too large
                 if constexpr (kSums) {
+                    constexpr int kPiece = RP >= 32 ? 32 : 16;
+                    const Two late2 = two(late, late);
 #pragma unroll
-                    for (int c = 0; c < RP / 16; ++c) {
-                        if (16 * c >= a.columns) break;
-                        uint32_t o[16];
-                        tmem_load(sums_at + 16 * c, o);
+                    for (int c = 0; c < RP / kPiece; ++c) {
+                        if (kPiece * c >= a.columns) break;
+                        uint32_t o[kPiece];
+                        tmem_load(sums_at + kPiece * c, o);
                         tmem_landed(o);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            sum[16 * c + r] = PASS == kByRows ? fmaf(late, __uint_as_float(o[r]), sum[16 * c + r]) : sum[16 * c + r] + __uint_as_float(o[r]);
+                        for (int r = 0; r < kPiece; r += 2) {
+                            const Two add = two(__uint_as_float(o[r]), __uint_as_float(o[r + 1])), old = two(sum[kPiece * c + r], sum[kPiece * c + r + 1]);
+                            const float2 v = both(PASS == kByRows ? fma2(late2, add, old) : add2(add, old));
+                            sum[kPiece * c + r] = v.x;
+                            sum[kPiece * c + r + 1] = v.y;
+                        }
                     }
                 }
             };
-            for (int64_t tile = t0; tile < t1; ++tile, ++seen, ++turns) {
+            for (int64_t tile = t0; tile < t1; ++tile, ++seen) {
                 const uint32_t b = seen % kBuffers, s_at = lanes + 128 * b + kHalf * h;
                 if (!arrived(&bars.scores[t][b], (seen / kBuffers) & 1)) break;
                 float late = 1.f;
                 const int valid = (int)min(a.n_other - tile * kTile - kHalf * h, (int64_t)kHalf);
-                const float *vec = reinterpret_cast<const float *>(smem + (other_at - own_at) + (turns % a.stages) * stage_bytes + KT * other_term) + kHalf * h;
-                if (PASS == kByColumns && !arrived(&bars.full[turns % a.stages], (turns / a.stages) & 1)) break;   // base and pull came with the tile
+                const float *vec = reinterpret_cast<const float *>(smem + (other_at - own_at) + place.at * stage_bytes + KT * other_term) + kHalf * h;
+                if (PASS == kByColumns) {                            // base and pull came with the tile
+                    if (!arrived(&bars.full[place.at], place.turn)) break;
+                    place.next(a.stages);
+                }
                 Two part[2] = {0, 0};
 #pragma unroll
                 for (int c = 0; c < kHalf / kStep; ++c) {
@@ -451,16 +484,17 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
                 }
                 if (kSums) {
                     if (tile > t0) {                                 // O of the tile before, which the next product overwrites
-                        if (!arrived(&bars.sums[t][h], (seen - 1) & 1)) break;
+                        if (kBuffers == 2 && !arrived(&bars.sums[t], (seen - 1) & 1)) break;
                         take(late);
                     }
                     tmem_stored();
                 }
                 fence_before();
                 __syncwarp();
-                if (lane == 0) arrive(smem_u32(&bars.shares[t][h][b]));
+                if (lane == 0) arrive(smem_u32(&bars.shares[t][b]));
             }
-            if (kSums && ok && arrived(&bars.sums[t][h], (seen - 1) & 1)) take(1.f);
+            if (kSums && ok && arrived(&bars.sums[t], (kBuffers == 2 ? seen - 1 : runs) & 1)) take(1.f);
+            ++runs;
             // Half 1 hands its sums to half 0 where O was: nothing writes there before the shares of half 1 in the next run.
             if (h == 1) {
                 if constexpr (kSums) {
