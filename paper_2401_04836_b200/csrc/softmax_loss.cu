@@ -451,7 +451,7 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     const int leaf = p.order - 1;
     const bool table = grad && p.grad[leaf];
     p.tensor = p.rank <= kTensorRank;
-    const int own = p.tensor ? tensor_rows(p.rank) : kTile, other = p.tensor ? kTensorTile : kTile, blocks = p.tensor ? 148 : 148 * 2;
+    const int own = p.tensor ? kTensorRows : kTile, other = p.tensor ? tensor_tile(p.rank, kWide) : kTile, blocks = p.tensor ? 148 : 148 * 2;
     const Split by_rows = split_units(p.fibres, own, p.columns, other, blocks);
     const Split by_columns = split_units(p.columns, own, p.fibres, other, blocks);
     const int columns = image_columns(p.rank), width = p.tensor ? columns : (p.rank + kTile - 1) / kTile * kTile;

@@ -123,8 +123,8 @@ struct Problem {
 
 // softmax_tensor.cu: rows of a group and of a tile, and one pass.  `wide`: factors in fp32 (three products a product, shares of
 // 22 bits), else in bf16 (shares of 11 bits).
-constexpr int kTensorTile = 128;
-int tensor_rows(int rank);                      // own rows of a group
+constexpr int kTensorRows = 256;                // own rows of a group
+int tensor_tile(int rank, bool wide);           // other rows of a tile
 cudaError_t tensor_pass(int pass, bool wide, const TensorArgs &a, int blocks, cudaStream_t stream);
 
 }  // namespace loss

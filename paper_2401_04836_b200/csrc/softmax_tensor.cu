@@ -24,12 +24,12 @@ namespace {
 using namespace umma;
 
 constexpr int kRows = 128;                       // of a tile of own rows: lanes of tensor memory
-constexpr int kMaxTiles = 2;                     // tiles of own rows a block has
-constexpr int kTile = 128;                       // other rows of a tile, half of them to each of two warpgroups
-constexpr int kHalf = kTile / 2;
+constexpr int kTiles = 2;                        // tiles of own rows a block has
+constexpr int kTeams = 2 * kTiles;               // warpgroups that make shares: two a tile, each with half of the other rows
+constexpr int kThreads = 128 * (kTeams + 1);
 constexpr int kMaxStages = 4;
 constexpr int kShift = 4;                        // shares are 2^kShift times too large: small ones stay in fp16's range
-constexpr float kSlack = 11.f;                   // by how much a score may exceed the base (2^(kShift + kSlack) < 65504)
+constexpr float kMostShares = 65504.f;           // no share of a tile exceeds fp16 if their sum does not
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -40,7 +40,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
 struct Barriers {
     uint64_t own_full, own_free;                 // own rows in shared memory: there, read for the last time
     uint64_t full[kMaxStages], free[kMaxStages]; // a tile of other rows
-    uint64_t done[2 * kMaxTiles];                // S of a warpgroup, and every product that it issued before, is complete
+    uint64_t done[kTeams][2];                    // S of a chain, and every product that it issued before, is complete (by buffer of S)
 };
 
 // A place in the ring of stages and the parity of its turn.
@@ -79,10 +79,12 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 }
 __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
 
-__host__ __device__ constexpr int tiles_of(int columns) { return columns <= 64 ? 2 : 1; }
-__host__ __device__ constexpr int threads_of(int columns) { return 128 * (2 * tiles_of(columns) + 1); }
-// whether tensor memory has room for the own rows' terms beside S and O
-__host__ __device__ constexpr bool own_in_tensor(int columns) { return columns != 64; }
+// Up to rank 32 each team is a chain of its own: scores, shares, sums.  Above, S and O are too wide for four of each in tensor
+// memory and the sums for the registers of every team: the two teams of a tile share S and O and split the columns of the sums.
+// Without sums they share S, of which there are two: the next one is made while this one is read.
+__host__ __device__ constexpr bool paired(int columns, int pass) { return columns > 32 || pass == kLossAlone; }
+// Tiles of 128 other rows, or of 64 where 256 own rows of two terms leave no room for two of 128.
+__host__ __device__ constexpr int tile_of(int columns, int terms) { return columns > 64 && terms == 4 ? 64 : 128; }
 
 // two fp32 values in one register pair: one instruction for both
 using Two = unsigned long long;
@@ -112,40 +114,66 @@ __device__ __forceinline__ Two mul2(Two a, Two b) {
     return r;
 }
 
+// The same value, made at this place.
+__device__ __forceinline__ uint32_t hidden(uint32_t x) {
+    uint32_t y;
+    asm volatile("mov.u32 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// What the fp16 pair lost of two fp32 values, as fp16.
+__device__ __forceinline__ uint32_t pack_lost(uint32_t hi, float2 v) {
+    const float2 f = unpack(hi);
+    const float2 l = both(fma2(two(f.x, f.y), two(-1.f, -1.f), two(v.x, v.y)));
+    return pack(l.x, l.y);
+}
+
+// Whether `v` holds in any of the N threads that come to this barrier.
+template <int N>
+__device__ __forceinline__ bool any_of(int barrier, bool v) {
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.aligned.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"((uint32_t)v), "r"(barrier), "n"(N) : "memory");
+    return any != 0;
+}
+
 // RP: room for sums in registers.  QT, KT: terms of own and other rows; PT: terms of a share (its product takes as many of Other).
 template <int RP, int PASS, int QT, int KT, int PT>
-__global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_constant__ TensorArgs a) {
-    constexpr bool kSums = PASS != kLossAlone;
-    constexpr int kTiles = tiles_of(RP);                             // tiles of own rows
-    constexpr int kTeams = 2 * kTiles;                               // warpgroups that make shares: two a tile, 64 other rows each
-    constexpr bool kOwnInTensor = own_in_tensor(RP);
-    // columns of tensor memory: S of every team (P takes its place), own rows of every tile, O of every team
-    constexpr int kOwnAt = kHalf * kTeams, kOwnWide = kOwnInTensor ? RP : 0;
+__global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant__ TensorArgs a) {
+    constexpr bool kSums = PASS != kLossAlone, kPaired = paired(RP, PASS);
+    constexpr int kTile = tile_of(RP, QT * KT), kHalf = kTile / 2;   // other rows of a tile, of a team
+    constexpr int kChains = kPaired ? kTiles : kTeams;               // what issues and waits for products of its own
+    // columns of tensor memory: S (P takes its place), own rows, O
+    constexpr int kBuffers = kSums ? 1 : 2;                          // of S
+    constexpr int kWide = kPaired ? kTile : kHalf;                   // of S of a chain
+    constexpr int kOwnAt = kWide * kBuffers * kChains, kOwnWide = kPaired ? 0 : RP;
     constexpr int kSumsAt = kOwnAt + kOwnWide * kTiles;
-    static_assert(kSumsAt + RP * kTeams <= 512);
-    constexpr int kStep = RP <= 32 ? 32 : 16;                        // scores a thread has in registers at once
+    static_assert(kSumsAt + (kSums ? RP * kChains : 0) <= 512);
+    constexpr int kMine = kPaired ? RP / 2 : RP;                     // columns of the sums that a thread adds up
+    constexpr int kStep = RP <= 32 ? 32 : 16;                        // scores a thread loads at once
+    constexpr int kSync = kPaired ? 256 : 128;                       // threads of a chain
     constexpr int kLoader = 4 * kTeams;                              // warp
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ Barriers bars;
-    __shared__ float2 merged[kTiles][kRows];                         // maximum and sum of the second team
+    __shared__ float told[kTiles][2][kRows];                         // what the teams of a tile tell each other
     __shared__ uint32_t tmem_at;
-    __shared__ int failed_s, team_gave_up[kTeams][2], tile_gave_up[kTiles];
+    __shared__ int failed_s, chain_gave_up[kChains][2], tile_gave_up[kTiles];
     volatile int *failed = &failed_s;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t row_bytes = 2u * a.columns;
     const uint32_t own_term = kRows * row_bytes, other_term = kTile * row_bytes;
     const uint32_t stage_bytes = KT * other_term + (PASS == kByColumns ? 8u * kTile : 0u);
-    const uint32_t own_at = smem_u32(smem), other_at = own_at + (kOwnInTensor ? 0 : kTiles * QT * own_term);
+    const uint32_t own_at = smem_u32(smem), other_at = own_at + (!kPaired ? 0 : kTiles * QT * own_term);
 
     if (threadIdx.x == 0) {
         failed_s = 0;
-        for (int w = 0; w < kTeams; ++w) team_gave_up[w][0] = team_gave_up[w][1] = 0;
+        for (int w = 0; w < kChains; ++w) chain_gave_up[w][0] = chain_gave_up[w][1] = 0;
         for (int t = 0; t < kTiles; ++t) tile_gave_up[t] = 0;
         auto init = [](uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_u32(b)), "r"(n) : "memory"); };
         init(&bars.own_full, 1);
-        init(&bars.own_free, kTeams);
-        for (int s = 0; s < kMaxStages; ++s) init(&bars.full[s], 1), init(&bars.free[s], kTeams);
-        for (int w = 0; w < kTeams; ++w) init(&bars.done[w], 1);
+        init(&bars.own_free, kChains);
+        for (int s = 0; s < kMaxStages; ++s) init(&bars.full[s], 1), init(&bars.free[s], kChains);
+        for (int w = 0; w < kChains; ++w) init(&bars.done[w][0], 1), init(&bars.done[w][1], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kLoader) {
@@ -158,40 +186,42 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
     const uint32_t tmem = tmem_at;
     after_last_kernel();
 
-    const int64_t u0 = (int64_t)blockIdx.x * a.each, u1 = min(u0 + a.each, a.groups * a.tiles);
+    // this block's units: `rest` of them from tile t0 of group g on
+    const int64_t u0 = (int64_t)blockIdx.x * a.each;
+    const int all_tiles = (int)a.tiles;
+    int g = (int)(u0 / all_tiles), t0 = (int)(u0 - (int64_t)g * all_tiles), rest = (int)min(a.each, a.groups * a.tiles - u0);
     if (warp >= kLoader) {
-        // of the launch's registers (5 x 96 or 3 x 168, by warpgroups) these warps leave the teams 4 x 112 or 2 x 224
-        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // of the launch's registers (96 a thread, 5 warpgroups) this warpgroup leaves the teams 4 x 112
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
         if (warp == kLoader && elect_one()) {
             Place place;
             uint32_t run = 0, loads = 0;                             // runs begun; tiles loaded, up to the number of stages
             bool ok = true;
-            for (int64_t u = u0; u < u1 && ok;) {
-                const int64_t g = u / a.tiles, t0 = u - g * a.tiles, t1 = min(a.tiles, t0 + (u1 - u));
-                if (!kOwnInTensor) {
-                    const int live = (int)min((a.n_own - g * kTiles * kRows + kRows - 1) / kRows, (int64_t)kTiles);
+            for (; rest > 0 && ok; ++g, t0 = 0) {
+                const int t1 = min(all_tiles, t0 + rest);
+                if (kPaired) {
+                    const int live = (int)min((a.n_own - (int64_t)g * kTiles * kRows + kRows - 1) / kRows, (int64_t)kTiles);
                     if (!(ok = wait_for(smem_u32(&bars.own_free), (run & 1) ^ 1, a.polls, failed))) break;
                     const uint32_t bar = smem_u32(&bars.own_full);
                     expect(bar, live * QT * own_term);
                     ++run;
                     for (int t = 0; t < live; ++t)
                         for (int q = 0; q < QT; ++q)
-                            bulk_load(own_at + (t * QT + q) * own_term, (q ? a.own.lo : a.own.hi) + (g * kTiles + t) * kRows * a.columns, own_term, bar);
+                            bulk_load(own_at + (t * QT + q) * own_term, (q ? a.own.lo : a.own.hi) + ((int64_t)g * kTiles + t) * kRows * a.columns, own_term, bar);
                 }
-                for (int64_t t = t0; t < t1; ++t) {
+                for (int t = t0; t < t1; ++t) {
                     if (!(ok = wait_for(smem_u32(&bars.free[place.at]), place.turn ^ 1, a.polls, failed))) break;
                     const uint32_t full = smem_u32(&bars.full[place.at]), to = other_at + place.at * stage_bytes;
                     expect(full, stage_bytes);
-                    for (int q = 0; q < KT; ++q) bulk_load(to + q * other_term, (q ? a.other.lo : a.other.hi) + t * kTile * a.columns, other_term, full);
+                    for (int q = 0; q < KT; ++q) bulk_load(to + q * other_term, (q ? a.other.lo : a.other.hi) + (int64_t)t * kTile * a.columns, other_term, full);
                     if (PASS == kByColumns) {
-                        bulk_load(to + KT * other_term, a.base + t * kTile, 4 * kTile, full);
-                        bulk_load(to + KT * other_term + 4 * kTile, a.pull + t * kTile, 4 * kTile, full);
+                        bulk_load(to + KT * other_term, a.base + (int64_t)t * kTile, 4 * kTile, full);
+                        bulk_load(to + KT * other_term + 4 * kTile, a.pull + (int64_t)t * kTile, 4 * kTile, full);
                     }
                     place.next(a.stages);
                     loads = min(loads + 1, (uint32_t)a.stages);
                 }
-                u += t1 - t0;
+                rest -= t1 - t0;
             }
             // nothing of this block is under way when it ends, whatever the others did
             if (!ok) {
@@ -205,116 +235,192 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
         }
         __syncwarp();
     } else {
-        if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
         const int team = warp / 4, t = team / 2, h = team % 2;       // tile of own rows, half of the other rows
-        const bool issues = warp % 4 == team;                        // the warp that issues the team's products: one on each scheduler
-        const uint32_t s_at = tmem + kHalf * team, own_tmem = tmem + kOwnAt + kOwnWide * t, sums_at = tmem + kSumsAt + RP * team;
-        const uint32_t lanes = (uint32_t)(warp % 4) << 21;           // 32 lanes a warp
-        const int in_tile = 32 * (warp % 4) + lane;
+        const int chain = kPaired ? t : team;
+        const bool issues = warp % 4 == team && (!kPaired || h == 0);                  // the warp that issues the chain's products: each on a scheduler of its own
+        const uint32_t lanes = tmem + ((uint32_t)(warp % 4) << 21);  // 32 lanes a warp
+        const uint32_t s_at = lanes + kWide * kBuffers * chain + (kPaired ? kHalf * h : 0), my_sums = lanes + kSumsAt + RP * chain + (kPaired ? kMine * h : 0);
+        const int in_tile = 32 * (warp % 4) + lane, barrier = kPaired ? 1 + t : 1 + kTiles + team;
         // from accumulated scores to units of log 2, and what undoes the scales of the sums
         const int e_own = image_exponent(a.words[a.own_word]), e_other = image_exponent(a.words[a.other_word]);
         const float unit = kLog2e * exp2f((float)-e_own) * exp2f((float)-e_other);
         const Two unit2 = two(unit, unit);
-        const uint32_t done = smem_u32(&bars.done[team]);
-        uint32_t turn = 0, runs = 0, beat = 0;                       // parity of `done`; runs; tiles
+        const uint32_t done = smem_u32(&bars.done[chain][0]);        // and 8 bytes further, of the second buffer
+        uint32_t turn = 0, runs = 0, beat = 0;                       // parity of `done` (one buffer); runs; tiles
         Place place;
         bool ok = true;
         auto arrived = [&](uint32_t bar, uint32_t parity) {          // for the whole warp or not at all
-            ok = __all_sync(0xffffffffu, wait_for(bar, parity, a.polls, failed));
+            ok = __all_sync(0xffffffffu, wait_for(bar, parity, a.polls, failed)) && ok;
             fence_after();
             return ok;
         };
-        // descriptors of the first 16 columns (scores) or rows (sums); further ones, terms and stages lie a constant apart
-        const uint32_t group_rows = 8 * row_bytes;                   // bytes of 8 rows: 8 columns of them are 128 bytes
-        const uint64_t own_k = smem_desc(own_at + t * QT * own_term, 128, group_rows);
-        const uint64_t other_k = smem_desc(other_at + h * kHalf * row_bytes, 128, group_rows), other_mn = smem_desc(other_at + h * kHalf * row_bytes, group_rows, 128);
-        const uint32_t q_term = own_term >> 4, k_term = other_term >> 4, k_stage = stage_bytes >> 4, mn_step = (2 * group_rows) >> 4;
-        const uint32_t i_scores = idesc_f16(kRows, kHalf, false), i_sums = idesc_f16(kRows, a.columns, true);
-        const int deep = a.columns / 16;
-        auto scores = [&](uint32_t stage) {
-            const uint64_t k = other_k + stage * k_stage;
+        // What issuing needs is made anew each time, from a number that the compiler cannot see through: kept, it would cost every
+        // thread some twenty registers.
+        auto scores = [&](uint32_t stage, uint32_t buffer) {
+            const uint32_t me = hidden(chain), to = tmem + kWide * (kBuffers * me + buffer);
+            const uint32_t group_rows = 16 * a.columns;              // bytes of 8 rows: 8 columns of them are 128 bytes
+            // descriptors of the first 16 columns; further ones and terms lie a constant apart
+            const uint64_t k = smem_desc(other_at + stage * stage_bytes + (kPaired ? 0 : me % 2 * kHalf * row_bytes), 128, group_rows);
+            const uint64_t q = smem_desc(own_at + me * QT * own_term, 128, group_rows);
+            const uint32_t own_tmem = tmem + kOwnAt + kOwnWide * (me / 2), k_term = other_term >> 4, q_term = own_term >> 4;
+            const int deep = a.columns / 16;
             if (!a.withhold && elect_one()) {
                 bool first = true;
-                auto product = [&](int q, uint64_t ka) {             // term q of own rows
+                auto product = [&](int term, uint64_t ka) {          // term of own rows
 #pragma unroll
                     for (int c = 0; c < RP / 16; ++c, first = false) {
                         if (c >= deep) break;
-                        if (kOwnInTensor) umma_f16_ts(s_at, own_tmem + q * (RP / 2) + 8 * c, ka + c * 16, i_scores, first ? 0u : 1u);
-                        else umma_f16(s_at, own_k + q * q_term + c * 16, ka + c * 16, i_scores, first ? 0u : 1u);
+                        if (!kPaired) umma_f16_ts(to, own_tmem + term * (RP / 2) + 8 * c, ka + c * 16, idesc_f16(kRows, kWide, false), first ? 0u : 1u);
+                        else umma_f16(to, q + term * q_term + c * 16, ka + c * 16, idesc_f16(kRows, kWide, false), first ? 0u : 1u);
                     }
                 };
                 if (QT == 2) product(1, k);
                 if (KT == 2) product(0, k + k_term);
                 product(0, k);
-                umma_commit(done);
+                umma_commit(done + 8 * buffer);
             }
             __syncwarp();
         };
         auto sums = [&](uint32_t stage, bool last) {
-            const uint64_t k = other_mn + stage * k_stage;
+            const uint32_t me = hidden(chain), p_at = tmem + kWide * me, to = tmem + kSumsAt + RP * me;
+            const uint32_t group_rows = 16 * a.columns, k_term = other_term >> 4, step = (2 * group_rows) >> 4, i_sums = idesc_f16(kRows, a.columns, true);
+            const uint64_t k = smem_desc(other_at + stage * stage_bytes + (kPaired ? 0 : me % 2 * kHalf * row_bytes), group_rows, 128);      // of the first 16 rows
             if (!a.withhold && elect_one()) {
                 bool first = true;
                 auto product = [&](uint32_t pa, uint64_t ka) {
 #pragma unroll
-                    for (int c = 0; c < kHalf / 16; ++c, first = false) umma_f16_ts(sums_at, pa + c * 16, ka + c * mn_step, i_sums, first ? 0u : 1u);
+                    for (int c = 0; c < kWide / 16; ++c, first = false) umma_f16_ts(to, pa + c * 16, ka + c * step, i_sums, first ? 0u : 1u);
                 };
-                if (kSums) {
-                    if (PT == 2) {
-                        product(s_at + 8, k);
-                        product(s_at, k + k_term);
-                    }
-                    product(s_at, k);
+                if (PT == 2) {
+                    product(p_at + 8, k);
+                    product(p_at, k + k_term);
                 }
+                product(p_at, k);
                 umma_commit(smem_u32(&bars.free[stage]));
                 if (last) umma_commit(done);
             }
             __syncwarp();
         };
-        for (int64_t u = u0; u < u1 && ok; ++runs) {
-            const int64_t g = u / a.tiles, t0 = u - g * a.tiles, t1 = min(a.tiles, t0 + (u1 - u));
-            if ((g * kTiles + t) * kRows >= a.n_own) {               // no such rows: only what the loader waits for
-                for (int64_t tile = t0; tile < t1 && ok; ++tile) {
+        for (int tiles; rest > 0 && ok; ++runs, ++g, t0 = 0, rest -= tiles) {
+            tiles = min(all_tiles - t0, rest);
+            if (((int64_t)g * kTiles + t) * kRows >= a.n_own) {      // no such rows: only what the loader waits for
+                for (int i = 0; i < tiles && ok; ++i) {
                     if (issues && arrived(smem_u32(&bars.full[place.at]), place.turn) && lane == 0) arrive(smem_u32(&bars.free[place.at]));
                     place.next(a.stages);
                 }
-                if (!kOwnInTensor && issues && lane == 0) arrive(smem_u32(&bars.own_free));
-                u += t1 - t0;
+                if (kPaired && issues && lane == 0) arrive(smem_u32(&bars.own_free));
                 continue;
             }
             float top = -INFINITY, total = 0.f;
-            float sum[kSums ? RP : 1];
+            float sum[kSums ? kMine : 1];
 #pragma unroll
-            for (int r = 0; r < (kSums ? RP : 1); ++r) sum[r] = 0.f;
-            auto take = [&](float late) {                            // adds O of a tile, made from shares `late` times too large
+            for (int r = 0; r < (kSums ? kMine : 1); ++r) sum[r] = 0.f;
+            auto take = [&] {                                        // adds O of a tile
                 if constexpr (kSums) {
-                    constexpr int kPiece = RP >= 32 ? 32 : 16;
-                    const Two late2 = two(late, late);
+                    constexpr int kPiece = kMine >= 32 ? 32 : 16;
 #pragma unroll
-                    for (int c = 0; c < RP / kPiece; ++c) {
-                        if (kPiece * c >= a.columns) break;
+                    for (int c = 0; c < kMine / kPiece; ++c) {
+                        if (kPiece * c + (kPaired ? kMine * h : 0) >= a.columns) break;
                         uint32_t o[kPiece];
-                        tmem_load(sums_at + lanes + kPiece * c, o);
+                        tmem_load(my_sums + kPiece * c, o);
                         tmem_landed(o);
 #pragma unroll
                         for (int r = 0; r < kPiece; r += 2) {
-                            const Two add = two(__uint_as_float(o[r]), __uint_as_float(o[r + 1])), old = two(sum[kPiece * c + r], sum[kPiece * c + r + 1]);
-                            const float2 v = both(PASS == kByRows ? fma2(late2, add, old) : add2(add, old));
+                            const float2 v = both(add2(two(sum[kPiece * c + r], sum[kPiece * c + r + 1]), two(__uint_as_float(o[r]), __uint_as_float(o[r + 1]))));
                             sum[kPiece * c + r] = v.x;
                             sum[kPiece * c + r + 1] = v.y;
                         }
                     }
                 }
             };
-            if constexpr (kOwnInTensor) {                            // a row a thread, one term a team
+            // Raises the base to the tile's maximum: at the first tile, and when shares came out too large for fp16.  Powers of two:
+            // nothing is rounded.  Two teams that share their products have one base.
+            auto raise = [&](uint32_t from, int valid) {
+                float m = -INFINITY;
+#pragma unroll 1
+                for (int c = 0; c < kHalf / 16; ++c) {
+                    uint32_t s[16];
+                    tmem_load(from + 16 * c, s);
+                    tmem_landed(s);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (16 * c + j < valid) m = fmaxf(m, __uint_as_float(s[j]));
+                }
+                float now = fmaxf(top, ceilf(m * unit));
+                if (kPaired && kSums) {
+                    told[t][h][in_tile] = now;
+                    asm volatile("bar.sync %0, 256;" :: "r"(1 + t) : "memory");
+                    now = fmaxf(now, told[t][1 - h][in_tile]);
+                }
+                const float keep = now > top ? exp2f(top - now) : 1.f;
+                top = now;
+                total *= keep;
+#pragma unroll
+                for (int r = 0; r < (kSums ? kMine : 1); ++r) sum[r] *= keep;
+            };
+            // Shares of a tile: their sum, and with sums their fp16 terms in the place of the scores, while the next scores load.
+            auto shares = [&](uint32_t from, int valid, const float *vec) {
+                // no score yet (a team without other rows): nothing to subtract, the shares are 2^-inf
+                const float base = top == -INFINITY ? 0.f : (kSums ? (float)kShift : 0.f) - top;
+                const Two base2 = two(base, base);
+                Two part[2] = {0, 0};
+                auto piece = [&](uint32_t (&now)[16], int c) {       // 16 scores
+                    uint32_t hi[8], lo[8];
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        Two p[2];
+                        ulonglong2 pull;
+                        if (PASS == kByColumns) {
+                            const ulonglong2 bs = *reinterpret_cast<const ulonglong2 *>(vec + 16 * c + 2 * j);
+                            pull = *reinterpret_cast<const ulonglong2 *>(vec + kTile + 16 * c + 2 * j);
+                            p[0] = bs.x;
+                            p[1] = bs.y;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const Two e = fma2(two(__uint_as_float(now[2 * (j + i)]), __uint_as_float(now[2 * (j + i) + 1])), unit2, PASS == kByColumns ? p[i] : base2);
+                            p[i] = two(exp2_fast(both(e).x), exp2_fast(both(e).y));
+                            if (PASS == kByColumns) p[i] = mul2(p[i], i ? pull.y : pull.x);
+                            else part[i] = add2(part[i], p[i]);
+                            if (!kSums) continue;
+                            const float2 v = both(p[i]);
+                            hi[j + i] = pack(v.x, v.y);
+                            if (PT == 2) lo[j + i] = pack_lost(hi[j + i], v);
+                        }
+                    }
+                    if (kSums) {
+                        tmem_store(from + 16 * c, hi);
+                        if (PT == 2) tmem_store(from + 16 * c + 8, lo);
+                    }
+                };
+                uint32_t s[kStep];
+#pragma unroll
+                for (int c = 0; c < kHalf / 16; ++c) {
+                    if (16 * c % kStep == 0) {
+                        tmem_load(from + 16 * c, s);
+                        tmem_landed(s);
+                        if (PASS != kByColumns && valid < kHalf) {   // the last tile of all
+                            asm volatile("" ::: "memory");           // a branch: not a select for every score of every tile
+#pragma unroll
+                            for (int j = 0; j < kStep; ++j)
+                                if (16 * c + j >= valid) s[j] = 0xff800000u;           // -inf
+                        }
+                    }
+                    piece(*reinterpret_cast<uint32_t(*)[16]>(s + 16 * c % kStep), c);
+                }
+                const float2 x = both(add2(part[0], part[1]));
+                return x.x + x.y;
+            };
+            if constexpr (!kPaired) {                            // a row a thread, one term a team
                 for (int q = h; q < QT; q += 2) {
-                    const uint4 *from = reinterpret_cast<const uint4 *>((q ? a.own.lo : a.own.hi) + ((g * kTiles + t) * kRows + in_tile / 8 * 8) * a.columns) + in_tile % 8;
+                    const uint4 *from = reinterpret_cast<const uint4 *>((q ? a.own.lo : a.own.hi) + (((int64_t)g * kTiles + t) * kRows + in_tile / 8 * 8) * a.columns) + in_tile % 8;
 #pragma unroll
                     for (int c = 0; c < RP / 16; ++c) {
-                        if (c >= deep) break;
+                        if (16 * c >= a.columns) break;
                         const uint4 x = __ldg(from + 16 * c), y = __ldg(from + 16 * c + 8);
                         const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                        tmem_store(own_tmem + lanes + q * (RP / 2) + 8 * c, w);
+                        tmem_store(lanes + kOwnAt + kOwnWide * t + q * (RP / 2) + 8 * c, w);
                     }
                 }
                 tmem_stored();
@@ -323,191 +429,145 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
                 fence_after();
             }
             if (issues) {
-                if ((kOwnInTensor || arrived(smem_u32(&bars.own_full), runs & 1)) && arrived(smem_u32(&bars.full[place.at]), place.turn)) scores(place.at);
+                if ((!kPaired || arrived(smem_u32(&bars.own_full), runs & 1)) && arrived(smem_u32(&bars.full[place.at]), place.turn)) scores(place.at, beat % kBuffers);
             }
-            for (int64_t tile = t0; tile < t1; ++tile, ++beat) {
-                if (arrived(done, turn)) {
-                    float late = 1.f;
-                    const int valid = (int)min(a.n_other - tile * kTile - kHalf * h, (int64_t)kHalf);
-                    const float *vec = reinterpret_cast<const float *>(smem + (other_at - own_at) + place.at * stage_bytes + KT * other_term) + kHalf * h;
-                    if (PASS == kByColumns) arrived(smem_u32(&bars.full[place.at]), place.turn);    // base and pull came with the tile
-                    Two part[2] = {0, 0};
-#pragma unroll
-                    for (int c = 0; c < kHalf / kStep; ++c) {
-                        uint32_t s[kStep];
-                        tmem_load(s_at + lanes + kStep * c, s);
-                        tmem_landed(s);
-                        if (PASS != kByColumns) {
-                            if (valid < kHalf)
-#pragma unroll
-                                for (int j = 0; j < kStep; ++j)
-                                    if (kStep * c + j >= valid) s[j] = 0xff800000u;    // -inf
-                            float m = __uint_as_float(s[0]);
-#pragma unroll
-                            for (int j = 1; j < kStep; ++j) m = fmaxf(m, __uint_as_float(s[j]));
-                            m *= unit;
-                            const bool raise = m > top + (PASS == kLossAlone ? 60.f : kSlack);
-                            if (__any_sync(0xffffffffu, raise)) {
-                                const float now = raise ? ceilf(m) : top, keep = raise ? exp2f(top - now) : 1.f;
-                                top = now;
-                                total *= keep;
-                                late *= keep;
-#pragma unroll
-                                for (int q = 0; q < 2; ++q) part[q] = mul2(part[q], two(keep, keep));
-                                if (kSums) {
-#pragma unroll
-                                    for (int r = 0; r < RP; ++r) sum[r] *= keep;
-#pragma unroll 1
-                                    for (int k = 0; k < c * kStep / 16; ++k) {          // shares of this tile that are written already
-                                        uint32_t p[16], w[8];
-                                        tmem_stored();
-                                        tmem_load(s_at + lanes + 16 * k, p);
-                                        tmem_landed(p);
-#pragma unroll
-                                        for (int j = 0; j < 8; ++j) {
-                                            float2 v = unpack(p[j]);
-                                            if (PT == 2) {
-                                                const float2 lo = unpack(p[8 + j]);
-                                                v.x = (v.x + lo.x) * keep;
-                                                v.y = (v.y + lo.y) * keep;
-                                            } else {
-                                                v.x *= keep;
-                                                v.y *= keep;
-                                            }
-                                            w[j] = pack(v.x, v.y);
-                                            const float2 hi = unpack(w[j]);
-                                            p[j] = pack(v.x - hi.x, v.y - hi.y);
-                                        }
-                                        tmem_store(s_at + lanes + 16 * k, w);
-                                        if (PT == 2) {
-#pragma unroll
-                                            for (int j = 0; j < 8; ++j) w[j] = p[j];
-                                            tmem_store(s_at + lanes + 16 * k + 8, w);
-                                        }
-                                    }
-                                }
-                            }
-                        }
-                        // no score yet (a half without other rows): nothing to subtract, the shares are 2^-inf
-                        const float base = top == -INFINITY ? 0.f : (PASS == kLossAlone ? 0.f : (float)kShift) - top;
-                        const Two base2 = two(base, base);
-#pragma unroll
-                        for (int k = 0; k < kStep / 16; ++k) {
-                            uint32_t hi[8], lo[8];
-#pragma unroll
-                            for (int j = 0; j < 8; j += 2) {
-                                const int at = 16 * k + 2 * j;
-                                Two p[2];
-                                ulonglong2 pull;
-                                if (PASS == kByColumns) {
-                                    const ulonglong2 bs = *reinterpret_cast<const ulonglong2 *>(vec + kStep * c + at);
-                                    pull = *reinterpret_cast<const ulonglong2 *>(vec + kTile + kStep * c + at);
-                                    p[0] = bs.x;
-                                    p[1] = bs.y;
-                                }
-#pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    const Two e = fma2(two(__uint_as_float(s[at + 2 * i]), __uint_as_float(s[at + 2 * i + 1])), unit2, PASS == kByColumns ? p[i] : base2);
-                                    p[i] = two(exp2_fast(both(e).x), exp2_fast(both(e).y));
-                                    if (PASS == kByColumns) p[i] = mul2(p[i], i ? pull.y : pull.x);
-                                    else part[i] = add2(part[i], p[i]);
-                                    if (!kSums) continue;
-                                    const float2 v = both(p[i]);
-                                    hi[j + i] = pack(v.x, v.y);
-                                    if (PT == 2) {
-                                        const float2 f = unpack(hi[j + i]);
-                                        const float2 l = both(fma2(two(f.x, f.y), two(-1.f, -1.f), p[i]));
-                                        lo[j + i] = pack(l.x, l.y);
-                                    }
-                                }
-                            }
-                            if (kSums) {
-                                tmem_store(s_at + lanes + kStep * c + 16 * k, hi);
-                                if (PT == 2) tmem_store(s_at + lanes + kStep * c + 16 * k + 8, lo);
-                            }
-                        }
+            bool low = true, fresh = false;                          // the base is not known to be high enough; O holds a tile's sums
+            for (int i = 0; i < tiles; ++i, ++beat) {
+                // A wait that gave up does not end the loop here: the barriers below want every warp.  What the tensor cores may still
+                // be writing is read then, and not used.
+                const uint32_t from = s_at + kWide * (beat % kBuffers), stage = place.at;
+                // how many of the team's other rows there are: only the last tile of all may lack some
+                const int valid = t0 + i + 1 < all_tiles ? kHalf : (int)min(a.n_other - (int64_t)(t0 + i) * kTile - kHalf * h, (int64_t)kHalf);
+                if (kBuffers == 2) {
+                    arrived(done + 8 * (beat & 1), beat / 2 & 1);
+                    // these scores are all that wanted the tile: the next ones are made while they are read
+                    place.next(a.stages);
+                    if (issues) {
+                        if (lane == 0) arrive(smem_u32(&bars.free[stage]));
+                        __syncwarp();
+                        if (i + 1 < tiles && arrived(smem_u32(&bars.full[place.at]), place.turn)) scores(place.at, (beat + 1) & 1);
                     }
-                    if (PASS != kByColumns) {
-                        const float2 x = both(add2(part[0], part[1]));
-                        total += x.x + x.y;
-                    }
-                    if (kSums) {
-                        if (tile > t0) take(late);                   // O of the tile before is complete: it was issued in front of these scores
-                        tmem_stored();
-                    }
+                } else {
+                    arrived(done, turn);
                     turn ^= 1;
                 }
-                fence_before();
-                if (!ok) *(volatile int *)&team_gave_up[team][beat & 1] = 1;
-                asm volatile("bar.sync %0, 128;" :: "r"(1 + kTiles + team) : "memory");
-                ok = *(volatile int *)&team_gave_up[team][beat & 1] == 0;        // the same for the whole team
-                const uint32_t stage = place.at;
-                place.next(a.stages);
+                const float *vec = reinterpret_cast<const float *>(smem + (other_at - own_at) + stage * stage_bytes + KT * other_term) + kHalf * h;
+                if (PASS == kByColumns) {
+                    arrived(smem_u32(&bars.full[stage]), place.turn);                  // base and pull came with the tile
+                    shares(from, valid, vec);
+                    if (i > 0) take();                               // O of the tile before is complete: it was issued in front of these scores
+                    tmem_stored();
+                    fence_before();
+                    if (!ok) *(volatile int *)&chain_gave_up[chain][beat & 1] = 1;
+                    asm volatile("bar.sync %0, %1;" :: "r"(barrier), "n"(kSync) : "memory");
+                    ok = *(volatile int *)&chain_gave_up[chain][beat & 1] == 0;        // the same for the whole chain
+                } else if (!kSums) {
+                    bool low = i == 0;
+                    float part;
+#pragma unroll 1
+                    do {
+                        if (low) raise(from, valid);
+                        part = shares(from, valid, vec);
+                        low = __any_sync(0xffffffffu, part > 0x1p100f);
+                    } while (low);
+                    total += part;
+                    fence_before();
+                    if (!ok) *(volatile int *)&chain_gave_up[chain][beat & 1] = 1;
+                    asm volatile("bar.sync %0, %1;" :: "r"(barrier), "n"(kSync) : "memory");
+                    ok = *(volatile int *)&chain_gave_up[chain][beat & 1] == 0;
+                } else {
+                    if (low) raise(from, valid);
+                    const float part = shares(from, valid, vec);
+                    if (fresh) take();
+                    tmem_stored();
+                    fence_before();
+                    if (!ok) *(volatile int *)&chain_gave_up[chain][beat & 1] = 1;
+                    low = any_of<kSync>(barrier, part > kMostShares);
+                    ok = *(volatile int *)&chain_gave_up[chain][beat & 1] == 0;
+                    fresh = !low;
+                    if (low && ok) {                                 // a share of the chain was too large: its scores once more, for a higher base
+                        fence_after();
+                        if (issues) scores(stage, 0);
+                        --i;
+                        continue;
+                    }
+                    total += part;
+                }
                 if (!ok) break;
-                if (issues) {
-                    fence_after();
-                    sums(stage, tile + 1 == t1);
-                    if (tile + 1 < t1 && arrived(smem_u32(&bars.full[place.at]), place.turn)) scores(place.at);   // behind the products that read the shares in their place
+                if (kSums) {
+                    place.next(a.stages);
+                    if (issues) {
+                        fence_after();
+                        sums(stage, i + 1 == tiles);
+                        if (i + 1 < tiles && arrived(smem_u32(&bars.full[place.at]), place.turn)) scores(place.at, 0);   // behind the products that read the shares in their place
+                    }
                 }
             }
-            if (ok && arrived(done, turn)) {
+            if (kSums && ok && arrived(done, turn)) {
                 turn ^= 1;
-                take(1.f);
+                take();
             }
-            // The second team hands its sums to the first where its O was.
+            // The second team tells the first its maximum and sum; without a product in common, it hands its sums over where its O was.
             if (h == 1) {
-                if constexpr (kSums) {
+                if constexpr (kSums && !kPaired) {
 #pragma unroll
                     for (int c = 0; c < RP / 8; ++c) {
                         if (8 * c >= a.columns) break;
                         uint32_t w[8];
 #pragma unroll
                         for (int r = 0; r < 8; ++r) w[r] = __float_as_uint(sum[8 * c + r]);
-                        tmem_store(sums_at + lanes + 8 * c, w);
+                        tmem_store(my_sums + 8 * c, w);
                     }
                     tmem_stored();
                 }
-                merged[t][in_tile] = make_float2(top, total);
+                told[t][0][in_tile] = top;
+                told[t][1][in_tile] = total;
                 fence_before();
             }
             if (!ok) *(volatile int *)&tile_gave_up[t] = 1;
             asm volatile("bar.sync %0, 256;" :: "r"(1 + t) : "memory");
             ok = *(volatile int *)&tile_gave_up[t] == 0;             // the same for both teams: both go on or neither
-            if (!kOwnInTensor && issues && lane == 0) arrive(smem_u32(&bars.own_free));    // every product of the team is complete
-            if (h == 0) {
-                fence_after();
-                const int64_t part = (g * a.parts + ((int64_t)blockIdx.x - g * a.tiles / a.each)) * (kTiles * kRows) + kRows * t + in_tile;
-                const float2 other = merged[t][in_tile];
-                const float shift = PASS == kByRows ? 1.f / (1 << kShift) : 1.f;
-                float mine = 1.f, theirs = 1.f;
-                if (PASS != kByColumns) {
-                    const float most = fmaxf(top, other.x);
-                    mine = top == -INFINITY ? 0.f : exp2f(top - most);
-                    theirs = other.x == -INFINITY ? 0.f : exp2f(other.x - most);
-                    a.top[part] = most;
-                    a.total[part] = (total * mine + other.y * theirs) * shift;
-                }
-                if constexpr (kSums) {
-                    const float undo = exp2f((float)-e_other) * shift, undo2 = PASS == kByColumns ? exp2f((float)-image_exponent(a.words[kMaxWeight])) : 1.f;
-                    float4 *to = reinterpret_cast<float4 *>(a.sum + part * a.width);
+            if (kPaired && issues && lane == 0) arrive(smem_u32(&bars.own_free));      // every product of the chain is complete
+            fence_after();
+            const int64_t part = ((int64_t)g * a.parts + ((int64_t)blockIdx.x - g * a.tiles / a.each)) * (kTiles * kRows) + kRows * t + in_tile;
+            const float shift = PASS == kByRows ? 1.f / (1 << kShift) : 1.f;
+            float mine = 1.f, theirs = 1.f;
+            if (PASS != kByColumns && h == 0) {
+                const float2 other = make_float2(told[t][0][in_tile], told[t][1][in_tile]);
+                const float most = fmaxf(top, other.x);
+                mine = top == -INFINITY ? 0.f : exp2f(top - most);
+                theirs = other.x == -INFINITY ? 0.f : exp2f(other.x - most);
+                a.top[part] = most;
+                a.total[part] = (total * mine + other.y * theirs) * shift;
+            }
+            if constexpr (kSums) {
+                const float undo = exp2f((float)-e_other) * shift, undo2 = PASS == kByColumns ? exp2f((float)-image_exponent(a.words[kMaxWeight])) : 1.f;
+                const int first = kPaired ? kMine * h : 0;
+                float4 *to = reinterpret_cast<float4 *>(a.sum + part * a.width + first);
+                if (kPaired || h == 0) {
 #pragma unroll
-                    for (int c = 0; c < RP / 16; ++c) {
-                        if (16 * c >= a.columns) break;
-                        uint32_t o[16];
-                        tmem_load(sums_at + RP + lanes + 16 * c, o);
-                        tmem_landed(o);
+                    for (int c = 0; c < kMine / 16; ++c) {
+                        if (16 * c + first >= a.columns) break;
                         float x[16];
+                        if constexpr (kPaired) {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) x[r] = fmaf(sum[16 * c + r], mine, __uint_as_float(o[r]) * theirs) * undo * undo2;
+                            for (int r = 0; r < 16; ++r) x[r] = sum[16 * c + r];
+                        } else {
+                            uint32_t o[16];
+                            tmem_load(my_sums + RP + 16 * c, o);
+                            tmem_landed(o);
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) to[4 * c + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                            for (int r = 0; r < 16; ++r) x[r] = fmaf(sum[16 * c + r], mine, __uint_as_float(o[r]) * theirs);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            to[4 * c + q] = make_float4(x[4 * q] * undo * undo2, x[4 * q + 1] * undo * undo2, x[4 * q + 2] * undo * undo2, x[4 * q + 3] * undo * undo2);
                     }
                 }
-                fence_before();
             }
+            fence_before();
             asm volatile("bar.sync %0, 256;" :: "r"(1 + t) : "memory");
             fence_after();
-            u += t1 - t0;
         }
     }
     fence_before();
@@ -521,7 +581,8 @@ __global__ void __launch_bounds__(threads_of(RP), 1) loss_tensor(const __grid_co
 template <int RP, int PASS, int QT, int KT, int PT>
 cudaError_t launch(TensorArgs a, int blocks, cudaStream_t stream) {
     constexpr int kMost = 224 * 1024;                                // of 227 KB: barriers and what halves exchange are apart
-    const int own = own_in_tensor(RP) ? 0 : tiles_of(RP) * QT * kRows * 2 * a.columns, stage = KT * kTile * 2 * a.columns + (PASS == kByColumns ? 8 * kTile : 0);
+    constexpr int kTile = tile_of(RP, QT * KT);
+    const int own = paired(RP, PASS) ? kTiles * QT * kRows * 2 * a.columns : 0, stage = KT * kTile * 2 * a.columns + (PASS == kByColumns ? 8 * kTile : 0);
     a.stages = std::min<int>(kMaxStages, (kMost - own) / stage);
     const int bytes = own + a.stages * stage;
     static PerDeviceOnce once;
@@ -529,7 +590,7 @@ cudaError_t launch(TensorArgs a, int blocks, cudaStream_t stream) {
         return cudaFuncSetAttribute(loss_tensor<RP, PASS, QT, KT, PT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     });
     if (e != cudaSuccess) return e;
-    return launch_early(loss_tensor<RP, PASS, QT, KT, PT>, dim3(blocks), threads_of(RP), bytes, stream, a);
+    return launch_early(loss_tensor<RP, PASS, QT, KT, PT>, dim3(blocks), kThreads, bytes, stream, a);
 }
 
 template <int RP, bool WIDE>
@@ -550,7 +611,7 @@ cudaError_t by_rank(int pass, const TensorArgs &a, int blocks, cudaStream_t stre
 
 }  // namespace
 
-int tensor_rows(int rank) { return kRows * tiles_of(image_columns(rank)); }
+int tensor_tile(int rank, bool wide) { return tile_of(image_columns(rank), wide ? 4 : 2); }
 
 cudaError_t tensor_pass(int pass, bool wide, const TensorArgs &a, int blocks, cudaStream_t stream) {
     return wide ? by_rank<true>(pass, a, blocks, stream) : by_rank<false>(pass, a, blocks, stream);
