@@ -14,7 +14,7 @@ namespace {
 constexpr int kWarp = 32;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / kWarp;
-constexpr int kRun = 64;           // leaves of a warp's run
+constexpr int kRun = 64;           // leaves of a fibre that one warp walks
 constexpr int kStrip = 128;        // columns of a row that a warp holds at once, 4 a lane
 
 __device__ __forceinline__ float value(const float *p, int64_t i) { return __ldg(p + i); }
@@ -26,12 +26,17 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// The last p in [0, n) with pos[p] <= at (pos ascends; every node has a child, so it is the node that holds `at`).
+// The last p in [0, n) with pos[p] <= at (pos ascends; every node has a child, so it is the node that holds `at`).  For a whole
+// warp: every step asks at 32 places, so a range of 32 000 nodes takes three loads one after another.
 __device__ __forceinline__ int32_t holder(const int32_t *__restrict__ pos, int64_t n, int64_t at) {
-    int64_t lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (__ldg(pos + mid) <= at) lo = mid; else hi = mid - 1;
+    const int lane = threadIdx.x % kWarp;
+    int64_t lo = 0;                                                    // pos[lo] <= at, and the answer is below lo + n
+    while (n > 1) {
+        const int64_t step = (n + kWarp) / (kWarp + 1), p = lo + (lane + 1) * step;
+        const bool below = p < lo + n && __ldg(pos + p) <= at;
+        const int64_t up = step * __popc(__ballot_sync(0xffffffffu, below));
+        lo += up;
+        n = min(step, n - up);
     }
     return (int32_t)lo;
 }
@@ -85,80 +90,84 @@ __device__ __forceinline__ void keep_largest(uint32_t *word, float v) {
     __syncthreads();
 }
 
-// One warp a fibre: its path and its row h, of which it returns the largest magnitude.
+// One warp, at most kRun leaves [first, last) of fibre f with path `at`: weight, target scores and, with a gradient, the targets'
+// share of it.  All leaves' rows are independent loads; sums leave the registers once.
 template <typename T>
-__device__ __forceinline__ float make_row(const Problem &p, int64_t f, float most) {
+__device__ __forceinline__ void walk_leaves(const Problem &p, const int32_t *at, int64_t f, int64_t first, int64_t last, bool grad) {
+    const int lane = threadIdx.x % kWarp, leaf = p.order - 1;
+    const T *table = static_cast<const T *>(p.factor[leaf]);
+    float *d_table = grad ? p.acc[leaf] : nullptr;
+    for (int strip = 0; strip < p.rank; strip += kStrip) {
+        float h[4], sum[4] = {0.f, 0.f, 0.f, 0.f}, score = 0.f, weight = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int r = strip + lane + kWarp * q;
+            h[q] = r < p.rank ? row_value<T>(p, at, r) : 0.f;
+        }
+        for (int64_t some = first; some < last; some += kWarp) {
+            const int n = (int)min(last - some, (int64_t)kWarp);
+            const float my_x = lane < n ? __ldg(p.x + some + lane) : 0.f;
+            const int32_t my_k = lane < n ? __ldg(p.crd[leaf] + some + lane) : 0;
+            weight += my_x;
+#pragma unroll 4
+            for (int e = 0; e < n; ++e) {
+                const float x = __shfl_sync(0xffffffffu, my_x, e);
+                const int64_t row = (int64_t)__shfl_sync(0xffffffffu, my_k, e) * p.rank;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = strip + lane + kWarp * q;
+                    if (r >= p.rank) continue;
+                    const float c = value(table, row + r);
+                    score = fmaf(x * h[q], c, score);
+                    sum[q] = fmaf(x, c, sum[q]);
+                    if (d_table) atomicAdd(d_table + row + r, -p.scale * x * h[q]);
+                }
+            }
+        }
+        score = warp_sum(score);
+        weight = warp_sum(weight);
+        if (lane == 0) {
+            atomicAdd(p.xs + f, score);
+            if (strip == 0) atomicAdd(p.weight + f, weight);
+        }
+        if (grad)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = strip + lane + kWarp * q;
+                if (r < p.rank) atomicAdd(p.xc + f * p.rank + r, sum[q]);
+            }
+    }
+}
+
+// One warp a fibre: its path, its row h (of which it returns the largest magnitude) and its first kRun leaves.
+template <typename T>
+__device__ __forceinline__ float make_row(const Problem &p, int64_t f, bool grad, float most) {
     const int lane = threadIdx.x % kWarp;
+    const int32_t *__restrict__ ends = p.pos[p.order - 1];
+    const int64_t first = __ldg(ends + f), last = __ldg(ends + f + 1);
     int32_t at[kMaxOrder - 1];
     path_of(p, f, at);
-    for (int l = lane; l + 1 < p.order; l += kWarp) p.path[l][f] = at[l];
+    for (int l = 0; l + 1 < p.order; ++l)
+        if (lane == l) p.path[l][f] = at[l];
     for (int r = lane; r < p.rank; r += kWarp) {
         const float h = row_value<T>(p, at, r);
         p.h[f * p.rank + r] = h;
         most = larger_finite(most, h);
     }
+    walk_leaves<T>(p, at, f, first, min(last, first + kRun), grad);
     return most;
 }
 
-// One warp a run of kRun leaves, whatever fibres they lie in: weights, target scores and, with a gradient, the targets' share of
-// it.  A fibre's sums leave the registers when the run leaves the fibre; only a fibre that is cut by the ends of runs gets
-// more than one addition.
+// One warp a run of kRun leaves: those among them that are not the first kRun of their fibre.  They can only be of the fibre that
+// holds the run's first leaf.
 template <typename T>
-__device__ __forceinline__ void walk_leaves(const Problem &p, int64_t first, int64_t last, bool grad) {
-    const int lane = threadIdx.x % kWarp;
-    const int fl = p.order - 2;                                      // level of the fibres
-    const int32_t *__restrict__ ends = p.pos[fl + 1];
-    const T *table = static_cast<const T *>(p.factor[fl + 1]);
-    float *d_table = grad ? p.acc[fl + 1] : nullptr;
-    for (int strip = 0; strip < p.rank; strip += kStrip) {
-        int64_t f = holder(ends, p.fibres, first), end = 0;
-        float h[4], sum[4] = {0.f, 0.f, 0.f, 0.f}, score = 0.f, weight = 0.f;
-        bool fresh = true;
-        for (int64_t e = first; e <= last; ++e) {
-            if (!fresh && (e == end || e == last)) {
-                score = warp_sum(score);
-                if (lane == 0) {
-                    atomicAdd(p.xs + f, score);
-                    if (strip == 0) atomicAdd(p.weight + f, weight);
-                }
-                if (grad)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int r = strip + lane + kWarp * q;
-                        if (r < p.rank) atomicAdd(p.xc + f * p.rank + r, sum[q]);
-                    }
-                score = weight = 0.f;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) sum[q] = 0.f;
-                ++f;
-                fresh = true;
-            }
-            if (e == last) break;
-            if (fresh) {
-                int32_t at[kMaxOrder - 1];
-                path_of(p, f, at);
-                end = __ldg(ends + f + 1);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int r = strip + lane + kWarp * q;
-                    h[q] = r < p.rank ? row_value<T>(p, at, r) : 0.f;
-                }
-                fresh = false;
-            }
-            const float x = __ldg(p.x + e);
-            const int64_t row = (int64_t)__ldg(p.crd[fl + 1] + e) * p.rank;
-            weight += x;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int r = strip + lane + kWarp * q;
-                if (r >= p.rank) continue;
-                const float c = value(table, row + r);
-                score = fmaf(x * h[q], c, score);
-                sum[q] = fmaf(x, c, sum[q]);
-                if (d_table) atomicAdd(d_table + row + r, -p.scale * x * h[q]);
-            }
-        }
-    }
+__device__ __forceinline__ void walk_run(const Problem &p, int64_t run, bool grad) {
+    const int32_t *__restrict__ ends = p.pos[p.order - 1];
+    const int64_t f = holder(ends, p.fibres, run), first = max(run, (int64_t)__ldg(ends + f) + kRun), last = min(run + kRun, (int64_t)__ldg(ends + f + 1));
+    if (first >= last) return;
+    int32_t at[kMaxOrder - 1];
+    path_of(p, f, at);
+    walk_leaves<T>(p, at, f, first, last, grad);
 }
 
 template <typename T>
@@ -168,12 +177,8 @@ __global__ void __launch_bounds__(kThreads) loss_prepare(const __grid_constant__
     const int64_t runs = (p.leaves + kRun - 1) / kRun;
     float most_h = 0.f, most_c = 0.f;
     for (int64_t i = me; i < p.fibres + runs; i += warps) {
-        if (i < p.fibres) {
-            most_h = make_row<T>(p, i, most_h);
-        } else {
-            const int64_t first = (i - p.fibres) * kRun;
-            walk_leaves<T>(p, first, min(first + (int64_t)kRun, p.leaves), grad);
-        }
+        if (i < p.fibres) most_h = make_row<T>(p, i, grad, most_h);
+        else walk_run<T>(p, (i - p.fibres) * kRun, grad);
     }
     if (p.tensor) {
         const T *table = static_cast<const T *>(p.factor[p.order - 1]);
@@ -356,78 +361,145 @@ __global__ void __launch_bounds__(kThreads) loss_flat(const __grid_constant__ Fl
 // joining the parts
 // ------------------------------------------------------------------------------------------------
 
-// One warp a fibre: its loss, and with a gradient dh scattered to the factors above the leaves.
-template <typename T>
+// The loss of every fibre, and with a gradient dh scattered to the factors above the leaves.  TEAM warps of a block have a fibre: one,
+// or all where there are many parts a fibre (few fibres, a long leaf mode).
+template <typename T, int TEAM>
 __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Problem p, const __grid_constant__ Parts parts, bool grad) {
+    __shared__ float shared_top[kWarps], shared_total[kWarps], shared_sum[TEAM > 1 ? kWarps : 1][kWarp];
     after_last_kernel();
-    const int lane = threadIdx.x % kWarp;
-    const int64_t warps = (int64_t)gridDim.x * kWarps;
+    const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp, member = warp % TEAM;
     const bool gave_up = p.words[kGaveUp] != 0;
     const float pull = p.tensor ? exp2f((float)image_exponent(p.words[kMaxWeight])) : 1.f;
-    for (int64_t f = (int64_t)blockIdx.x * kWarps + threadIdx.x / kWarp; f < p.fibres; f += warps) {
+    const int64_t step = (int64_t)gridDim.x * (kWarps / TEAM);
+    for (int64_t f = (int64_t)blockIdx.x * (kWarps / TEAM) + warp / TEAM; f < p.fibres; f += step) {
         const int64_t g = f / parts.split.rows, row = f - g * parts.split.rows, first = g * parts.split.parts;
         const int n = parts.split.parts_of(g);
+        const float *tops = parts.top + first * parts.split.rows + row, *totals = parts.total + first * parts.split.rows + row;
         float top = -INFINITY, total = 0.f;
-        bool bad = gave_up;
-        for (int s = 0; s < n; ++s) {
-            const float t = parts.top[(first + s) * parts.split.rows + row];
-            top = fmaxf(top, t);
-            bad |= t != t;
+        for (int s = member * kWarp + lane; s < n; s += TEAM * kWarp) top = fmaxf(top, tops[(int64_t)s * parts.split.rows]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (TEAM > 1) {
+            if (lane == 0) shared_top[warp] = top;
+            __syncthreads();
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, shared_top[w]);
         }
-        for (int s = 0; s < n; ++s) {
-            const int64_t at = (first + s) * parts.split.rows + row;
-            total += parts.total[at] * exp2f(parts.top[at] - top);
+        for (int s = member * kWarp + lane; s < n; s += TEAM * kWarp) {
+            const float t = tops[(int64_t)s * parts.split.rows];
+            total += totals[(int64_t)s * parts.split.rows] * (t == top ? 1.f : exp2f(t - top));
+        }
+        total = warp_sum(total);
+        if (TEAM > 1) {
+            if (lane == 0) shared_total[warp] = total;
+            __syncthreads();
+            total = 0.f;
+            for (int w = 0; w < kWarps; ++w) total += shared_total[w];
         }
         const float w = p.weight[f];
-        if (bad) total = NAN;
-        if (lane == 0) {
+        if (gave_up) total = NAN;
+        if (lane == 0 && member == 0) {
             p.out[f] = w * fmaf(top, kLn2, logf(total)) - p.xs[f];
             if (grad) p.base[f] = -top, p.pull[f] = w / total * pull;
         }
-        if (!grad) continue;
-        int32_t at[kMaxOrder - 1];
-        for (int l = 0; l + 1 < p.order; ++l) at[l] = p.path[l][f];
-        const float share = w / total;
-        for (int r = lane; r < p.rank; r += kWarp) {
-            float sum = 0.f;
-            for (int s = 0; s < n; ++s) {
-                const int64_t part = (first + s) * parts.split.rows + row;
-                sum = fmaf(parts.sum[part * parts.width + r], exp2f(parts.top[part] - top), sum);
-            }
-            const float dh = p.scale * (share * sum - p.xc[f * p.rank + r]);
-            for (int l = 0; l + 1 < p.order; ++l) {
-                if (!p.acc[l]) continue;
-                float d = dh;
-                for (int m = 0; m + 1 < p.order; ++m)
-                    if (m != l) d *= value(static_cast<const T *>(p.factor[m]), (int64_t)at[m] * p.rank + r);
-                atomicAdd(p.acc[l] + (int64_t)at[l] * p.rank + r, d);
+        if (grad) {
+            int32_t at[kMaxOrder - 1];
+            for (int l = 0; l + 1 < p.order; ++l) at[l] = p.path[l][f];
+            const float share = w / total;
+            for (int r0 = 0; r0 < p.rank; r0 += kWarp) {
+                const int r = r0 + lane;
+                float sum = 0.f;
+                if (r < p.rank) {
+#pragma unroll 4
+                    for (int s = member; s < n; s += TEAM) {
+                        const float t = tops[(int64_t)s * parts.split.rows];
+                        sum = fmaf(parts.sum[((first + s) * parts.split.rows + row) * parts.width + r], t == top ? 1.f : exp2f(t - top), sum);
+                    }
+                }
+                if (TEAM > 1) {
+                    shared_sum[warp][lane] = sum;
+                    __syncthreads();
+                    sum = 0.f;
+                    for (int o = 0; o < kWarps; ++o) sum += shared_sum[o % TEAM][lane];
+                }
+                // the factors' rows are dealt to the members
+                if (r < p.rank) {
+                    const float dh = p.scale * (share * sum - p.xc[f * p.rank + r]);
+                    for (int l = member; l + 1 < p.order; l += TEAM) {
+                        if (!p.acc[l]) continue;
+                        float d = dh;
+                        for (int m = 0; m + 1 < p.order; ++m)
+                            if (m != l) d *= value(static_cast<const T *>(p.factor[m]), (int64_t)at[m] * p.rank + r);
+                        atomicAdd(p.acc[l] + (int64_t)at[l] * p.rank + r, d);
+                    }
+                }
+                if (TEAM > 1) __syncthreads();
             }
         }
+        if (TEAM > 1) __syncthreads();
     }
     start_next_kernel();
 }
 
+// N values at once, N = 4 where rows are multiples of 4 (and so 16-byte aligned in fp32).
+template <int N>
+__device__ __forceinline__ void load_values(const float *from, float (&v)[N]) {
+    if constexpr (N == 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(from);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+    } else {
+        v[0] = *from;
+    }
+}
+template <int N>
+__device__ __forceinline__ void store_values(float *to, const float (&v)[N]) {
+    if constexpr (N == 4) *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    else *to = v[0];
+}
+template <int N>
+__device__ __forceinline__ void store_values(__nv_bfloat16 *to, const float (&v)[N]) {
+    if constexpr (N == 4) {
+        const __nv_bfloat162 x[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+        *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(x);
+    } else {
+        *to = __float2bfloat16_rn(v[0]);
+    }
+}
+
 // The gradient of the leaf mode's factor from its parts, and every gradient in the type that was asked for.
-template <typename T>
+template <typename T, int N>
 __global__ void __launch_bounds__(kThreads) loss_finish(const __grid_constant__ Problem p, const __grid_constant__ Parts parts) {
     after_last_kernel();
     start_next_kernel();
     const int64_t me = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
-    const int leaf = p.order - 1;
+    const int leaf = p.order - 1, groups = p.rank / N;
     const float gave_up = p.words[kGaveUp] ? NAN : 0.f;
     if (p.grad[leaf])
-        for (int64_t e = me; e < p.extent[leaf] * p.rank; e += all) {
-            const int64_t k = e / p.rank, r = e - k * p.rank;
+        for (int64_t e = me; e < p.extent[leaf] * groups; e += all) {
+            const int64_t k = e / groups;
+            const int r = (int)(e - k * groups) * N;
             const int64_t g = k / parts.split.rows, row = k - g * parts.split.rows, first = g * parts.split.parts;
             const int n = parts.split.parts_of(g);
-            float sum = 0.f;
-            for (int s = 0; s < n; ++s) sum += parts.sum[((first + s) * parts.split.rows + row) * parts.width + r];
-            static_cast<T *>(p.grad[leaf])[e] = T(p.acc[leaf][e] + p.scale * sum + gave_up);
+            float sum[N] = {}, part[N];
+            for (int s = 0; s < n; ++s) {
+                load_values<N>(parts.sum + ((first + s) * parts.split.rows + row) * parts.width + r, part);
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += part[i];
+            }
+            load_values<N>(p.acc[leaf] + e * N, part);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] = part[i] + p.scale * sum[i] + gave_up;
+            store_values<N>(static_cast<T *>(p.grad[leaf]) + e * N, sum);
         }
     if (sizeof(T) < sizeof(float) || gave_up != 0.f)
         for (int l = 0; l < leaf; ++l)
             if (p.grad[l])
-                for (int64_t e = me; e < p.extent[l] * p.rank; e += all) static_cast<T *>(p.grad[l])[e] = T(p.acc[l][e] + gave_up);
+                for (int64_t e = me; e < p.extent[l] * groups; e += all) {
+                    float v[N];
+                    load_values<N>(p.acc[l] + e * N, v);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[i] += gave_up;
+                    store_values<N>(static_cast<T *>(p.grad[l]) + e * N, v);
+                }
 }
 
 int blocks_for(int64_t items, int per_block) {
@@ -526,12 +598,19 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
         }
     };
     pass(grad ? kByRows : kLossAlone, rows);
-    CB_LAUNCH("loss_rows", stream, ok(launch_early(loss_rows<T>, blocks_for(p.fibres, kWarps), kThreads, 0, stream, p, rows, grad)));
+    // many parts a fibre: a block for each (77 fibres of 148 parts, rank 64: 67 us with a warp each)
+    if (by_rows.parts > 16)
+        CB_LAUNCH("loss_rows", stream, ok(launch_early(loss_rows<T, kWarps>, blocks_for(p.fibres, 1), kThreads, 0, stream, p, rows, grad)));
+    else
+        CB_LAUNCH("loss_rows", stream, ok(launch_early(loss_rows<T, 1>, blocks_for(p.fibres, kWarps), kThreads, 0, stream, p, rows, grad)));
     if (table) pass(kByColumns, cols);
     if (grad) {
         int64_t most = 0;
         for (int l = 0; l <= leaf; ++l) most = std::max(most, p.extent[l] * p.rank);
-        CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T>, blocks_for(most, kThreads), kThreads, 0, stream, p, cols)));
+        if (p.rank % 4 == 0)
+            CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T, 4>, blocks_for(most / 4, kThreads), kThreads, 0, stream, p, cols)));
+        else
+            CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T, 1>, blocks_for(most, kThreads), kThreads, 0, stream, p, cols)));
     }
     ok(cudaFreeAsync(base, stream));
     return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
