@@ -28,7 +28,8 @@ constexpr int kTiles = 2;                        // tiles of own rows a block ha
 constexpr int kTeams = 2 * kTiles;               // warpgroups that make shares: two a tile, each with half of the other rows
 constexpr int kThreads = 128 * (kTeams + 1);
 constexpr int kMaxStages = 4;
-constexpr int kShift = 4;                        // shares are 2^kShift times too large: small ones stay in fp16's range
+constexpr int kShift = 5;                        // shares are 2^kShift times too large: small ones stay in fp16's range
+constexpr float kRoom = 3.f;                     // the first base is 2^kRoom above the first tile's largest share: most rows need no higher one
 constexpr float kMostShares = 65504.f;           // no share of a tile exceeds fp16 if their sum does not
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -77,7 +78,6 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-__device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
 
 // Up to rank 32 each team is a chain of its own: scores, shares, sums.  Above, S and O are too wide for four of each in tensor
 // memory and the sums for the registers of every team: the two teams of a tile share S and O and split the columns of the sums.
@@ -121,12 +121,8 @@ __device__ __forceinline__ uint32_t hidden(uint32_t x) {
     return y;
 }
 
-// What the fp16 pair lost of two fp32 values, as fp16.
-__device__ __forceinline__ uint32_t pack_lost(uint32_t hi, float2 v) {
-    const float2 f = unpack(hi);
-    const float2 l = both(fma2(two(f.x, f.y), two(-1.f, -1.f), two(v.x, v.y)));
-    return pack(l.x, l.y);
-}
+// The 11 leading bits of a positive value: exact in fp16 where that is not subnormal.
+__device__ __forceinline__ float leading(float v) { return __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
 
 // Whether `v` holds in any of the N threads that come to this barrier.
 template <int N>
@@ -312,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                 if (kPaired && issues && lane == 0) arrive(smem_u32(&bars.own_free));
                 continue;
             }
-            float top = -INFINITY, total = 0.f;
+            float top = -INFINITY, total = 0.f, fall = 1.f;          // fall: what a higher base makes of the sums so far, at the next addition
             float sum[kSums ? kMine : 1];
 #pragma unroll
             for (int r = 0; r < (kSums ? kMine : 1); ++r) sum[r] = 0.f;
@@ -327,11 +323,13 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                         tmem_landed(o);
 #pragma unroll
                         for (int r = 0; r < kPiece; r += 2) {
-                            const float2 v = both(add2(two(sum[kPiece * c + r], sum[kPiece * c + r + 1]), two(__uint_as_float(o[r]), __uint_as_float(o[r + 1]))));
+                            const Two old = two(sum[kPiece * c + r], sum[kPiece * c + r + 1]), add = two(__uint_as_float(o[r]), __uint_as_float(o[r + 1]));
+                            const float2 v = both(PASS == kByRows ? fma2(old, two(fall, fall), add) : add2(old, add));
                             sum[kPiece * c + r] = v.x;
                             sum[kPiece * c + r + 1] = v.y;
                         }
                     }
+                    fall = 1.f;
                 }
             };
             // Raises the base to the tile's maximum: at the first tile, and when shares came out too large for fp16.  Powers of two:
@@ -347,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                     for (int j = 0; j < 16; ++j)
                         if (16 * c + j < valid) m = fmaxf(m, __uint_as_float(s[j]));
                 }
-                float now = fmaxf(top, ceilf(m * unit));
+                float now = fmaxf(top, ceilf(m * unit) + (kSums && top == -INFINITY ? kRoom : 0.f));
                 if (kPaired && kSums) {
                     told[t][h][in_tile] = now;
                     asm volatile("bar.sync %0, 256;" :: "r"(1 + t) : "memory");
@@ -356,8 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                 const float keep = now > top ? exp2f(top - now) : 1.f;
                 top = now;
                 total *= keep;
-#pragma unroll
-                for (int r = 0; r < (kSums ? kMine : 1); ++r) sum[r] *= keep;
+                fall *= keep;
             };
             // Shares of a tile: their sum, and with sums their fp16 terms in the place of the scores, while the next scores load.
             auto shares = [&](uint32_t from, int valid, const float *vec) {
@@ -385,8 +382,14 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                             else part[i] = add2(part[i], p[i]);
                             if (!kSums) continue;
                             const float2 v = both(p[i]);
-                            hi[j + i] = pack(v.x, v.y);
-                            if (PT == 2) lo[j + i] = pack_lost(hi[j + i], v);
+                            if (PT == 2) {                           // cut, not rounded: one step less in front of the second term
+                                const float2 f = make_float2(leading(v.x), leading(v.y));
+                                const float2 l = both(fma2(two(f.x, f.y), two(-1.f, -1.f), p[i]));
+                                hi[j + i] = pack(f.x, f.y);
+                                lo[j + i] = pack(l.x, l.y);
+                            } else {
+                                hi[j + i] = pack(v.x, v.y);
+                            }
                         }
                     }
                     if (kSums) {
