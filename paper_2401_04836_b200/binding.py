@@ -458,31 +458,42 @@ def const_softmax_loss(csf: CsfHandle, factors, loss, grads=None, scale: float =
     _check(lib.const_softmax_loss(csf.ptr, ptrs, rank, kind, float(scale), at, outs, _stream_int(stream)), "const_softmax_loss")
 
 
+_clip_calls = None
+
+
 def const_clip_gradients(grads, max_norm: float, norm, out=None, stream=None) -> None:
     """Scales `grads` (CUDA tensors of one type: float32, float64 or bfloat16) so that their global norm is at most max_norm.
 
     norm: CUDA tensor of one value (float32; float64 for float64 gradients), receives the norm before the scaling.
     out: None (in place), or one tensor like each of `grads`.  A norm that is not finite scales nothing.
     """
-    import torch
+    global _clip_calls
     lib = _lib or load_library()
+    if _clip_calls is None:
+        import operator
+        from torch import Tensor, float32, float64
+        _clip_calls = Tensor.data_ptr, Tensor.numel, Tensor.is_contiguous, Tensor.get_device, operator.attrgetter("dtype"), float32, float64
+    data_ptr, numel, is_contiguous, get_device, dtype_of, float32, float64 = _clip_calls
     n = len(grads)
-    kind = _dtype_of(grads[0], (F32, F64, BF16)) if n else F32
-    outs = grads if out is None else out
-    if len(outs) != n:
+    if out is not None and len(out) != n:
         raise ValueError("out must have one entry per gradient")
-    for g, o in zip(grads, outs):
-        if not g.is_cuda or not g.is_contiguous() or g.dtype != grads[0].dtype:
-            raise ValueError("gradients must be contiguous CUDA tensors of one type")
-        if o is not g and (not o.is_cuda or not o.is_contiguous() or o.dtype != g.dtype or o.shape != g.shape):
-            raise ValueError("out must hold tensors like the gradients")
-    if not norm.is_cuda or norm.numel() != 1 or norm.dtype != (torch.float64 if kind == F64 else torch.float32):
+    # one pass of C calls over all tensors a check: there may be hundreds
+    tensors = grads if out is None else [*grads, *out]
+    kind = F32
+    if n:
+        types, devices = set(map(dtype_of, tensors)), set(map(get_device, tensors))
+        if len(types) != 1 or len(devices) != 1 or min(devices) < 0 or not all(map(is_contiguous, tensors)):
+            raise ValueError("gradients (and out) must be contiguous CUDA tensors of one type on one device")
+        kind = _dtype_of(grads[0], (F32, F64, BF16))
+    sizes = list(map(numel, grads))
+    if out is not None and list(map(numel, out)) != sizes:
+        raise ValueError("out must hold tensors like the gradients")
+    if norm.get_device() < 0 or norm.numel() != 1 or norm.dtype != (float64 if kind == F64 else float32):
         raise ValueError("norm must be a CUDA tensor of one float32 (float64 for float64 gradients)")
-    src = (ctypes.c_void_p * max(n, 1))(*[g.data_ptr() for g in grads])
-    dst = None if out is None else (ctypes.c_void_p * max(n, 1))(*[o.data_ptr() for o in outs])
-    sizes = (ctypes.c_int64 * max(n, 1))(*[g.numel() for g in grads])
-    _check(lib.const_clip_gradients(n, src, dst, sizes, kind, float(max_norm), norm.data_ptr(), _stream_int(stream)),
-           "const_clip_gradients")
+    many = ctypes.c_void_p * max(n, 1)
+    ptrs = list(map(data_ptr, tensors))
+    _check(lib.const_clip_gradients(n, many(*ptrs[:n]), None if out is None else many(*ptrs[n:]), (ctypes.c_int64 * max(n, 1))(*sizes), kind,
+                                    max_norm, norm.data_ptr(), _stream_int(stream)), "const_clip_gradients")
 
 
 def const_plan_set_tensor_stage(plan: PlanHandle, enable: bool) -> None:

@@ -15,15 +15,17 @@ namespace cb {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 768;              // tensors a launch: their table is a kernel argument (32 KB at most)
+constexpr int kMostTensors = 768;        // of a launch: their table is a kernel argument (32 KB at most)
 constexpr int kUnroll = 4;               // 16-byte loads a thread has under way
 constexpr int kBlocks = 148 * 8;         // also the number of partial sums
 
+// The tensors of a launch; of three sizes, since an argument is copied at every launch.
+template <int N>
 struct Table {
-    const void *in[kBatch];
-    void *out[kBatch];
-    int64_t n[kBatch];
-    int32_t chunk[kBatch + 1];           // first chunk of a tensor
+    const void *in[N];
+    void *out[N];
+    int64_t n[N];
+    int32_t chunk[N + 1];                // first chunk of a tensor
     int count;
     int blocks;                          // of the sum: partial sums to add up (of earlier launches too)
     int first;                           // where this launch's partial sums begin
@@ -32,7 +34,8 @@ struct Table {
 template <typename T>
 __host__ __device__ constexpr int chunk_values() { return kThreads * kUnroll * (16 / (int)sizeof(T)); }
 
-__device__ __forceinline__ int tensor_of(const Table &t, int c) {
+template <int N>
+__device__ __forceinline__ int tensor_of(const Table<N> &t, int c) {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -43,12 +46,53 @@ __device__ __forceinline__ int tensor_of(const Table &t, int c) {
 
 template <typename T> struct Wide { static constexpr int kN = 16 / (int)sizeof(T); T v[kN]; };
 
+// Values [0, n) of a chunk that starts at `in`, as a thread holds them: kUnroll times 16 bytes, the loads all under way at once; zeros
+// behind the end.
 template <typename T>
-__device__ __forceinline__ Wide<T> load_wide(const T *p) {
-    const uint4 raw = __ldg(reinterpret_cast<const uint4 *>(p));
-    Wide<T> w;
-    memcpy(&w, &raw, 16);
-    return w;
+__device__ __forceinline__ void load_chunk(const T *in, int n, Wide<T> (&w)[kUnroll]) {
+    constexpr int kWide = Wide<T>::kN;
+    if ((reinterpret_cast<uintptr_t>(in) & 15u) == 0) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int at = (u * kThreads + threadIdx.x) * kWide;
+            if (at + kWide <= n) {
+                const uint4 raw = *reinterpret_cast<const uint4 *>(in + at);
+                memcpy(&w[u], &raw, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kWide; ++i) w[u].v[i] = at + i < n ? in[at + i] : T(0.f);
+            }
+        }
+    } else {                             // any address: neighbours read neighbours
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) {
+                const int at = (u * kWide + i) * kThreads + threadIdx.x;
+                w[u].v[i] = at < n ? in[at] : T(0.f);
+            }
+    }
+}
+// The same values to `out`, which the chunk was loaded for: the way back is the way of the load.
+template <typename T>
+__device__ __forceinline__ void store_chunk(T *out, int n, const Wide<T> (&w)[kUnroll], bool wide) {
+    constexpr int kWide = Wide<T>::kN;
+    const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const int at = (u * kThreads + threadIdx.x) * kWide;
+        if (wide && aligned && at + kWide <= n) {
+            uint4 raw;
+            memcpy(&raw, &w[u], 16);
+            *reinterpret_cast<uint4 *>(out + at) = raw;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWide; ++i) {
+                const int one = wide ? at + i : (u * kWide + i) * kThreads + (int)threadIdx.x;
+                if (one < n) out[one] = w[u].v[i];
+            }
+        }
+    }
 }
 __device__ __forceinline__ float as_number(float x) { return x; }
 __device__ __forceinline__ double as_number(double x) { return x; }
@@ -75,9 +119,9 @@ __device__ __forceinline__ double squares(const T (&v)[N]) {
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) clip_sum(const __grid_constant__ Table t, double *__restrict__ partial) {
-    constexpr int kWide = Wide<T>::kN, kChunk = chunk_values<T>();
+template <typename T, int N>
+__global__ void __launch_bounds__(kThreads) clip_sum(const __grid_constant__ Table<N> t, double *__restrict__ partial) {
+    constexpr int kChunk = chunk_values<T>();
     after_last_kernel();
     __shared__ double warp_sums[kThreads / 32];
     double sum = 0.0;
@@ -85,20 +129,10 @@ __global__ void __launch_bounds__(kThreads) clip_sum(const __grid_constant__ Tab
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         const int at = tensor_of(t, c);
         const int64_t first = (int64_t)(c - t.chunk[at]) * kChunk;
-        const T *in = static_cast<const T *>(t.in[at]) + first;
-        const int64_t n = min(t.n[at] - first, (int64_t)kChunk);
-        if (n == kChunk && (reinterpret_cast<uintptr_t>(in) & 15u) == 0) {
-            Wide<T> w[kUnroll];
+        Wide<T> w[kUnroll];
+        load_chunk(static_cast<const T *>(t.in[at]) + first, (int)min(t.n[at] - first, (int64_t)kChunk), w);
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) w[u] = load_wide(in + (u * kThreads + threadIdx.x) * kWide);
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) sum += squares(w[u].v);
-        } else {
-            for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-                const T one[1] = {in[i]};
-                sum += squares(one);
-            }
-        }
+        for (int u = 0; u < kUnroll; ++u) sum += squares(w[u].v);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -112,11 +146,11 @@ __global__ void __launch_bounds__(kThreads) clip_sum(const __grid_constant__ Tab
     start_next_kernel();
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) clip_scale(const __grid_constant__ Table t, const double *__restrict__ partial, double max_norm,
+template <typename T, int N>
+__global__ void __launch_bounds__(kThreads) clip_scale(const __grid_constant__ Table<N> t, const double *__restrict__ partial, double max_norm,
                                                        void *norm_out) {
     using Number = std::conditional_t<sizeof(T) == 8, double, float>;
-    constexpr int kWide = Wide<T>::kN, kChunk = chunk_values<T>();
+    constexpr int kChunk = chunk_values<T>();
     after_last_kernel();
     start_next_kernel();
     __shared__ double warp_sums[kThreads / 32];
@@ -140,31 +174,21 @@ __global__ void __launch_bounds__(kThreads) clip_scale(const __grid_constant__ T
         if (!scales && t.out[at] == t.in[at]) continue;
         const int64_t first = (int64_t)(c - t.chunk[at]) * kChunk;
         const T *in = static_cast<const T *>(t.in[at]) + first;
-        T *out = static_cast<T *>(t.out[at]) + first;
-        const int64_t n = min(t.n[at] - first, (int64_t)kChunk);
-        if (n == kChunk && ((reinterpret_cast<uintptr_t>(in) | reinterpret_cast<uintptr_t>(out)) & 15u) == 0) {
-            uint4 raw[kUnroll];
+        const int n = (int)min(t.n[at] - first, (int64_t)kChunk);
+        Wide<T> w[kUnroll];
+        load_chunk(in, n, w);
+        if (scales)
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) raw[u] = *reinterpret_cast<const uint4 *>(in + (u * kThreads + threadIdx.x) * kWide);
+            for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                Wide<T> w;
-                memcpy(&w, &raw[u], 16);
-                if (scales)
-#pragma unroll
-                    for (int i = 0; i < kWide; ++i) w.v[i] = (T)(as_number(w.v[i]) * factor);
-                memcpy(&raw[u], &w, 16);
-                *reinterpret_cast<uint4 *>(out + (u * kThreads + threadIdx.x) * kWide) = raw[u];
-            }
-        } else {
-            for (int64_t i = threadIdx.x; i < n; i += kThreads) out[i] = scales ? (T)(as_number(in[i]) * factor) : in[i];
-        }
+                for (int i = 0; i < Wide<T>::kN; ++i) w[u].v[i] = (T)(as_number(w[u].v[i]) * factor);
+        store_chunk(static_cast<T *>(t.out[at]) + first, n, w, (reinterpret_cast<uintptr_t>(in) & 15u) == 0);
     }
 }
 
-template <typename T>
+template <typename T, int N>
 const_status_t run(int count, const void *const *in, void *const *out, const int64_t *sizes, double max_norm, void *norm, cudaStream_t stream) {
-    const int batches = std::max(1, (count + kBatch - 1) / kBatch);
+    const int batches = std::max(1, (count + N - 1) / N);
     double *partial = nullptr;
     if (scratch_alloc((void **)&partial, sizeof(double) * (size_t)kBlocks * batches, stream) != cudaSuccess) {
         (void)cudaGetLastError();                                      // the next launch must not find this error
@@ -172,11 +196,11 @@ const_status_t run(int count, const void *const *in, void *const *out, const int
     }
     cudaError_t e = cudaSuccess;
     int sums = 0;
-    Table t;
+    Table<N> t;
     auto fill = [&](int b) {
         t.count = 0;
         int64_t chunks = 0;
-        for (int i = b * kBatch; i < std::min(count, (b + 1) * kBatch); ++i) {
+        for (int i = b * N; i < std::min(count, (b + 1) * N); ++i) {
             if (sizes[i] == 0) continue;
             t.in[t.count] = in[i];
             t.out[t.count] = out[i];
@@ -191,12 +215,12 @@ const_status_t run(int count, const void *const *in, void *const *out, const int
         const int blocks = fill(b);
         t.first = sums;
         sums += blocks;
-        CB_LAUNCH("clip_sum", stream, e = launch_early(clip_sum<T>, blocks, kThreads, 0, stream, t, partial));
+        CB_LAUNCH("clip_sum", stream, e = launch_early(clip_sum<T, N>, blocks, kThreads, 0, stream, t, partial));
     }
     t.blocks = sums;
     for (int b = batches - 1; b >= 0 && e == cudaSuccess; --b) {       // the last batch is the one that L2 still holds
         const int blocks = fill(b);
-        CB_LAUNCH("clip_scale", stream, e = launch_early(clip_scale<T>, blocks, kThreads, 0, stream, t, (const double *)partial, max_norm, b == 0 ? norm : nullptr));
+        CB_LAUNCH("clip_scale", stream, e = launch_early(clip_scale<T, N>, blocks, kThreads, 0, stream, t, (const double *)partial, max_norm, b == 0 ? norm : nullptr));
     }
     if (cudaFreeAsync(partial, stream) != cudaSuccess || e != cudaSuccess) return CONST_ERR_CUDA;
     return CONST_OK;
@@ -210,9 +234,13 @@ const_status_t run_clip_gradients(int count, const void *const *in, void *const 
     int64_t total = 0;
     for (int i = 0; i < count; ++i) total += sizes[i] / 1024 + 1;
     if (total >= 2147483647ll) return CONST_ERR_UNSUPPORTED;
-    if (dtype == CONST_F32) return run<float>(count, in, out, sizes, max_norm, norm, stream);
-    if (dtype == CONST_F64) return run<double>(count, in, out, sizes, max_norm, norm, stream);
-    return run<__nv_bfloat16>(count, in, out, sizes, max_norm, norm, stream);
+    auto sized = [&](auto one) {
+        using T = decltype(one);
+        if (count <= 16) return run<T, 16>(count, in, out, sizes, max_norm, norm, stream);
+        if (count <= 128) return run<T, 128>(count, in, out, sizes, max_norm, norm, stream);
+        return run<T, kMostTensors>(count, in, out, sizes, max_norm, norm, stream);
+    };
+    return dtype == CONST_F32 ? sized(float()) : dtype == CONST_F64 ? sized(double()) : sized(__nv_bfloat16());
 }
 
 }  // namespace cb

@@ -374,6 +374,9 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
     for (int64_t f = (int64_t)blockIdx.x * (kWarps / TEAM) + warp / TEAM; f < p.fibres; f += step) {
         const int64_t g = f / parts.split.rows, row = f - g * parts.split.rows, first = g * parts.split.parts;
         const int n = parts.split.parts_of(g);
+        const float w = p.weight[f], score = p.xs[f];
+        int32_t at[kMaxOrder - 1];
+        for (int l = 0; l + 1 < p.order; ++l) at[l] = grad ? p.path[l][f] : 0;
         const float *tops = parts.top + first * parts.split.rows + row, *totals = parts.total + first * parts.split.rows + row;
         float top = -INFINITY, total = 0.f;
         for (int s = member * kWarp + lane; s < n; s += TEAM * kWarp) top = fmaxf(top, tops[(int64_t)s * parts.split.rows]);
@@ -395,15 +398,12 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
             total = 0.f;
             for (int w = 0; w < kWarps; ++w) total += shared_total[w];
         }
-        const float w = p.weight[f];
         if (gave_up) total = NAN;
         if (lane == 0 && member == 0) {
-            p.out[f] = w * fmaf(top, kLn2, logf(total)) - p.xs[f];
+            p.out[f] = w * fmaf(top, kLn2, logf(total)) - score;
             if (grad) p.base[f] = -top, p.pull[f] = w / total * pull;
         }
         if (grad) {
-            int32_t at[kMaxOrder - 1];
-            for (int l = 0; l + 1 < p.order; ++l) at[l] = p.path[l][f];
             const float share = w / total;
             for (int r0 = 0; r0 < p.rank; r0 += kWarp) {
                 const int r = r0 + lane;
@@ -465,26 +465,34 @@ __device__ __forceinline__ void store_values(__nv_bfloat16 *to, const float (&v)
     }
 }
 
-// The gradient of the leaf mode's factor from its parts, and every gradient in the type that was asked for.
-template <typename T, int N>
+// The gradient of the leaf mode's factor from its parts, and every gradient in the type that was asked for.  MANY: a warp has N values
+// and its lanes share the parts.
+template <typename T, int N, bool MANY>
 __global__ void __launch_bounds__(kThreads) loss_finish(const __grid_constant__ Problem p, const __grid_constant__ Parts parts) {
     after_last_kernel();
     start_next_kernel();
     const int64_t me = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
     const int leaf = p.order - 1, groups = p.rank / N;
+    constexpr int kLanes = MANY ? kWarp : 1;
+    const int member = MANY ? threadIdx.x % kWarp : 0;
     const float gave_up = p.words[kGaveUp] ? NAN : 0.f;
     if (p.grad[leaf])
-        for (int64_t e = me; e < p.extent[leaf] * groups; e += all) {
+        for (int64_t e = me / kLanes; e < p.extent[leaf] * groups; e += all / kLanes) {
             const int64_t k = e / groups;
             const int r = (int)(e - k * groups) * N;
             const int64_t g = k / parts.split.rows, row = k - g * parts.split.rows, first = g * parts.split.parts;
             const int n = parts.split.parts_of(g);
             float sum[N] = {}, part[N];
-            for (int s = 0; s < n; ++s) {
+#pragma unroll 2
+            for (int s = member; s < n; s += kLanes) {
                 load_values<N>(parts.sum + ((first + s) * parts.split.rows + row) * parts.width + r, part);
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[i] += part[i];
             }
+            if (MANY)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] = warp_sum(sum[i]);
+            if (member) continue;
             load_values<N>(p.acc[leaf] + e * N, part);
 #pragma unroll
             for (int i = 0; i < N; ++i) sum[i] = part[i] + p.scale * sum[i] + gave_up;
@@ -607,10 +615,15 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     if (grad) {
         int64_t most = 0;
         for (int l = 0; l <= leaf; ++l) most = std::max(most, p.extent[l] * p.rank);
-        if (p.rank % 4 == 0)
-            CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T, 4>, blocks_for(most / 4, kThreads), kThreads, 0, stream, p, cols)));
+        auto finish = [&](auto kernel, int64_t threads) {
+            CB_LAUNCH("loss_finish", stream, ok(launch_early(kernel, blocks_for(threads, kThreads), kThreads, 0, stream, p, cols)));
+        };
+        // many parts (a short leaf mode, many fibres): a warp for each value (200 rows of 123 parts at rank 8: 30 us with a thread each)
+        const int64_t values = p.rank % 4 == 0 ? most / 4 : most;
+        if (table && by_columns.parts > 16)
+            p.rank % 4 == 0 ? finish(loss_finish<T, 4, true>, values * kWarp) : finish(loss_finish<T, 1, true>, values * kWarp);
         else
-            CB_LAUNCH("loss_finish", stream, ok(launch_early(loss_finish<T, 1>, blocks_for(most, kThreads), kThreads, 0, stream, p, cols)));
+            p.rank % 4 == 0 ? finish(loss_finish<T, 4, false>, values) : finish(loss_finish<T, 1, false>, values);
     }
     ok(cudaFreeAsync(base, stream));
     return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
