@@ -297,7 +297,8 @@ const_status_t const_softmax_loss(const const_csf_t *csf, const void *const *fac
  * max_norm >= 0; infinity scales nothing.  A norm that is not finite scales nothing either: the values come through
  * as they are, and the caller sees the norm and drops the step.
  * Squares are added in fp32 over at most 8 values and in fp64 above that, in an order that only the sizes decide: the same call
- * gives the same bits.  Scratch (some 10 KB) as for const_execute; without it CONST_ERR_CUDA.  Asynchronous on `stream`; may be captured.
+ * gives the same bits.  Above some 130 000 values scratch (10 KB) as for const_execute; without it CONST_ERR_CUDA.  Asynchronous on `stream`;
+ * may be captured.
  */
 const_status_t const_clip_gradients(int n, const void *const *grads_dev, void *const *out_dev, const int64_t *sizes,
                                     const_dtype_t dtype, double max_norm, void *norm_dev, void *stream);

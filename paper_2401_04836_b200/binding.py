@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from array import array
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -96,7 +97,7 @@ def load_library():
     lib.const_plan_set_generic_executor.restype = i32
     lib.const_softmax_loss.argtypes = [vp, pp(vp), i32, i32, ctypes.c_double, vp, pp(vp), vp]
     lib.const_softmax_loss.restype = i32
-    lib.const_clip_gradients.argtypes = [i32, pp(vp), pp(vp), pp(i64), i32, ctypes.c_double, vp, vp]
+    lib.const_clip_gradients.argtypes = [i32, vp, vp, vp, i32, ctypes.c_double, vp, vp]
     lib.const_clip_gradients.restype = i32
     lib.const_destroy.argtypes = [vp]
     lib.const_destroy.restype = None
@@ -490,10 +491,10 @@ def const_clip_gradients(grads, max_norm: float, norm, out=None, stream=None) ->
         raise ValueError("out must hold tensors like the gradients")
     if norm.get_device() < 0 or norm.numel() != 1 or norm.dtype != (float64 if kind == F64 else float32):
         raise ValueError("norm must be a CUDA tensor of one float32 (float64 for float64 gradients)")
-    many = ctypes.c_void_p * max(n, 1)
-    ptrs = list(map(data_ptr, tensors))
-    _check(lib.const_clip_gradients(n, many(*ptrs[:n]), None if out is None else many(*ptrs[n:]), (ctypes.c_int64 * max(n, 1))(*sizes), kind,
-                                    max_norm, norm.data_ptr(), _stream_int(stream)), "const_clip_gradients")
+    ptrs, counts = array("Q", map(data_ptr, tensors)), array("q", sizes)
+    at = ptrs.buffer_info()[0]
+    _check(lib.const_clip_gradients(n, at, None if out is None else at + 8 * n, counts.buffer_info()[0], kind, max_norm, norm.data_ptr(),
+                                    _stream_int(stream)), "const_clip_gradients")
 
 
 def const_plan_set_tensor_stage(plan: PlanHandle, enable: bool) -> None:

@@ -34,12 +34,15 @@ struct Table {
 template <typename T>
 __host__ __device__ constexpr int chunk_values() { return kThreads * kUnroll * (16 / (int)sizeof(T)); }
 
+// The tensor of chunk c, from the chunks' table in shared memory; a warp asks at 32 places at once.
 template <int N>
-__device__ __forceinline__ int tensor_of(const Table<N> &t, int c) {
-    int lo = 0, hi = t.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (t.chunk[mid] <= c) lo = mid; else hi = mid - 1;
+__device__ __forceinline__ int tensor_of(const int32_t *chunk, int count, int c) {
+    int lo = 0, n = count;
+    while (n > 1) {
+        const int step = (n + 32) / 33, at = lo + ((int)(threadIdx.x % 32) + 1) * step;
+        const int up = step * __popc(__ballot_sync(0xffffffffu, at < lo + n && chunk[at] <= c));
+        lo += up;
+        n = min(step, n - up);
     }
     return lo;
 }
@@ -119,84 +122,147 @@ __device__ __forceinline__ double squares(const T (&v)[N]) {
     }
 }
 
+// The sum of `v` over the block, in the same order in every run.
+__device__ __forceinline__ double block_sum(double v, double *warp_sums) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (threadIdx.x % 32 == 0) warp_sums[threadIdx.x / 32] = v;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) s += warp_sums[w];
+    return s;
+}
+
+// One chunk as a kernel goes through them.
+template <typename T, int N>
+struct Chunk {
+    const T *in;
+    T *out;
+    int n;
+    __device__ __forceinline__ Chunk(const Table<N> &t, const int32_t *chunk, int c) {
+        const int at = tensor_of<N>(chunk, t.count, c);
+        const int64_t first = (int64_t)(c - chunk[at]) * chunk_values<T>();
+        in = static_cast<const T *>(t.in[at]) + first;
+        out = static_cast<T *>(t.out[at]) + first;
+        n = (int)min(t.n[at] - first, (int64_t)chunk_values<T>());
+    }
+};
+
+// norm and factor from a sum of squares; a norm that is no finite number scales nothing: the caller sees it and drops the step
+template <typename Number>
+struct Scale {
+    double norm;
+    bool scales;
+    Number factor;
+    __device__ __forceinline__ Scale(double sum, double max_norm) : norm(sqrt(sum)) {
+        scales = norm > max_norm && isfinite(norm);
+        factor = scales ? (Number)(max_norm / norm) : (Number)1;
+    }
+};
+
+template <typename T, typename Number>
+__device__ __forceinline__ void scale_values(Wide<T> (&w)[kUnroll], const Scale<Number> &s) {
+    if (!s.scales) return;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+        for (int i = 0; i < Wide<T>::kN; ++i) w[u].v[i] = (T)(as_number(w[u].v[i]) * s.factor);
+}
+template <typename T>
+using NumberOf = std::conditional_t<sizeof(T) == 8, double, float>;
+
 template <typename T, int N>
 __global__ void __launch_bounds__(kThreads) clip_sum(const __grid_constant__ Table<N> t, double *__restrict__ partial) {
-    constexpr int kChunk = chunk_values<T>();
-    after_last_kernel();
     __shared__ double warp_sums[kThreads / 32];
+    __shared__ int32_t chunk[N + 1];
+    for (int i = threadIdx.x; i <= t.count; i += kThreads) chunk[i] = t.chunk[i];
+    __syncthreads();
+    after_last_kernel();
     double sum = 0.0;
-    const int chunks = t.chunk[t.count];
+    const int chunks = chunk[t.count];
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int at = tensor_of(t, c);
-        const int64_t first = (int64_t)(c - t.chunk[at]) * kChunk;
+        const Chunk<T, N> at(t, chunk, c);
         Wide<T> w[kUnroll];
-        load_chunk(static_cast<const T *>(t.in[at]) + first, (int)min(t.n[at] - first, (int64_t)kChunk), w);
+        load_chunk(at.in, at.n, w);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) sum += squares(w[u].v);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (threadIdx.x % 32 == 0) warp_sums[threadIdx.x / 32] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double s = 0.0;
-        for (int w = 0; w < kThreads / 32; ++w) s += warp_sums[w];
-        partial[t.first + blockIdx.x] = s;
-    }
+    sum = block_sum(sum, warp_sums);
+    if (threadIdx.x == 0) partial[t.first + blockIdx.x] = sum;
     start_next_kernel();
 }
 
 template <typename T, int N>
 __global__ void __launch_bounds__(kThreads) clip_scale(const __grid_constant__ Table<N> t, const double *__restrict__ partial, double max_norm,
                                                        void *norm_out) {
-    using Number = std::conditional_t<sizeof(T) == 8, double, float>;
-    constexpr int kChunk = chunk_values<T>();
+    __shared__ double warp_sums[kThreads / 32];
+    __shared__ int32_t chunk[N + 1];
+    for (int i = threadIdx.x; i <= t.count; i += kThreads) chunk[i] = t.chunk[i];
+    __syncthreads();
     after_last_kernel();
     start_next_kernel();
-    __shared__ double warp_sums[kThreads / 32];
     double sum = 0.0;
     for (int i = threadIdx.x; i < t.blocks; i += kThreads) sum += partial[i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (threadIdx.x % 32 == 0) warp_sums[threadIdx.x / 32] = sum;
+    const Scale<NumberOf<T>> s(block_sum(sum, warp_sums), max_norm);
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *static_cast<NumberOf<T> *>(norm_out) = (NumberOf<T>)s.norm;
+    for (int c = chunk[t.count] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+        const Chunk<T, N> at(t, chunk, c);
+        if (!s.scales && at.out == at.in) continue;
+        Wide<T> w[kUnroll];
+        load_chunk(at.in, at.n, w);
+        scale_values(w, s);
+        store_chunk(at.out, at.n, w, (reinterpret_cast<uintptr_t>(at.in) & 15u) == 0);
+    }
+}
+
+// Few values: one cluster does both steps, its blocks telling each other their sums through shared memory -- one launch, no scratch.
+constexpr int kCluster = 8;
+constexpr int kClusterChunks = 4 * kCluster;           // up to so many chunks (131 072 fp32 values); 19 MB take longer than on all SMs
+
+template <typename T, int N>
+__global__ void __cluster_dims__(kCluster) __launch_bounds__(kThreads) clip_few(const __grid_constant__ Table<N> t, double max_norm, void *norm_out) {
+    __shared__ double warp_sums[kThreads / 32], sums[kCluster];
+    __shared__ int32_t chunk[N + 1];
+    for (int i = threadIdx.x; i <= t.count; i += kThreads) chunk[i] = t.chunk[i];
     __syncthreads();
+    after_last_kernel();
+    start_next_kernel();
+    const int chunks = chunk[t.count];
+    double sum = 0.0;
+    Wide<T> w[kUnroll];
+    for (int c = blockIdx.x; c < chunks; c += kCluster) {
+        const Chunk<T, N> at(t, chunk, c);
+        load_chunk(at.in, at.n, w);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) sum += squares(w[u].v);
+    }
+    sum = block_sum(sum, warp_sums);
+    if (threadIdx.x < kCluster) {
+        uint32_t there;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x])), "r"(threadIdx.x));
+        asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(there), "d"(sum) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) sum += warp_sums[w];
-    const double norm = sqrt(sum);
-    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *static_cast<Number *>(norm_out) = (Number)norm;
-    // a norm that is no finite number scales nothing: the caller sees it and drops the step
-    const bool scales = norm > max_norm && isfinite(norm);
-    const Number factor = scales ? (Number)(max_norm / norm) : (Number)1;
-    const int chunks = t.chunk[t.count];
-    for (int c = chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-        const int at = tensor_of(t, c);
-        if (!scales && t.out[at] == t.in[at]) continue;
-        const int64_t first = (int64_t)(c - t.chunk[at]) * kChunk;
-        const T *in = static_cast<const T *>(t.in[at]) + first;
-        const int n = (int)min(t.n[at] - first, (int64_t)kChunk);
-        Wide<T> w[kUnroll];
-        load_chunk(in, n, w);
-        if (scales)
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-                for (int i = 0; i < Wide<T>::kN; ++i) w[u].v[i] = (T)(as_number(w[u].v[i]) * factor);
-        store_chunk(static_cast<T *>(t.out[at]) + first, n, w, (reinterpret_cast<uintptr_t>(in) & 15u) == 0);
+    for (int b = 0; b < kCluster; ++b) sum += sums[b];
+    const Scale<NumberOf<T>> s(sum, max_norm);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *static_cast<NumberOf<T> *>(norm_out) = (NumberOf<T>)s.norm;
+    for (int c = blockIdx.x; c < chunks; c += kCluster) {
+        const Chunk<T, N> at(t, chunk, c);
+        if (!s.scales && at.out == at.in) continue;
+        if (chunks > kCluster) load_chunk(at.in, at.n, w);             // else the values are still here
+        scale_values(w, s);
+        store_chunk(at.out, at.n, w, (reinterpret_cast<uintptr_t>(at.in) & 15u) == 0);
     }
 }
 
 template <typename T, int N>
 const_status_t run(int count, const void *const *in, void *const *out, const int64_t *sizes, double max_norm, void *norm, cudaStream_t stream) {
     const int batches = std::max(1, (count + N - 1) / N);
-    double *partial = nullptr;
-    if (scratch_alloc((void **)&partial, sizeof(double) * (size_t)kBlocks * batches, stream) != cudaSuccess) {
-        (void)cudaGetLastError();                                      // the next launch must not find this error
-        return CONST_ERR_CUDA;
-    }
-    cudaError_t e = cudaSuccess;
-    int sums = 0;
     Table<N> t;
+    cudaError_t e = cudaSuccess;
     auto fill = [&](int b) {
         t.count = 0;
         int64_t chunks = 0;
@@ -211,6 +277,19 @@ const_status_t run(int count, const void *const *in, void *const *out, const int
         t.chunk[t.count] = (int32_t)chunks;
         return (int)std::max<int64_t>(1, std::min<int64_t>(chunks, kBlocks));
     };
+    if (batches == 1) {
+        fill(0);
+        if (t.chunk[t.count] <= kClusterChunks) {
+            CB_LAUNCH("clip_few", stream, e = launch_early(clip_few<T, N>, kCluster, kThreads, 0, stream, t, max_norm, norm));
+            return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
+        }
+    }
+    double *partial = nullptr;
+    if (scratch_alloc((void **)&partial, sizeof(double) * (size_t)kBlocks * batches, stream) != cudaSuccess) {
+        (void)cudaGetLastError();                                      // the next launch must not find this error
+        return CONST_ERR_CUDA;
+    }
+    int sums = 0;
     for (int b = 0; b < batches && e == cudaSuccess; ++b) {
         const int blocks = fill(b);
         t.first = sums;

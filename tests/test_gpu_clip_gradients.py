@@ -134,13 +134,16 @@ def test_refusals():
 
 
 def test_without_scratch():
-    grads, norm = make([100, 20], torch.float32), torch.full((1,), 7.0, device="cuda")
-    before = [g.clone() for g in grads]
+    """Few values need none; more are refused, and nothing is written."""
+    few, many = make([100, 20], torch.float32), make([300_000, 20], torch.float32)
+    norm, before = torch.full((1,), 7.0, device="cuda"), [g.clone() for g in many]
+    out = [torch.empty_like(g) for g in few]
     cb.const_debug_set(3, 1)
     try:
+        check(few, out, clip(few, 0.1, out), 0.1)
         with pytest.raises(cb.ConstError) as e:
-            cb.const_clip_gradients(grads, 0.1, norm)
+            cb.const_clip_gradients(many, 0.1, norm)
         assert e.value.status == 7
     finally:
         cb.const_debug_set(3, 0)
-    assert float(norm) == 7.0 and all(torch.equal(a, b) for a, b in zip(grads, before))
+    assert float(norm) == 7.0 and all(torch.equal(a, b) for a, b in zip(many, before))
