@@ -17,7 +17,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostTensors = 768;        // of a launch: their table is a kernel argument (32 KB at most)
 constexpr int kUnroll = 4;               // 16-byte loads a thread has under way
-constexpr int kBlocks = 148 * 8;         // also the number of partial sums
+constexpr int kPerSm = 4;                // blocks of the sum on an SM; and of the scaling (489 M fp32 values: 3 take 665 us, 4 715, 6 743: fewer
+constexpr int kScalePerSm = 3;           // streams of reads and writes at once)
+constexpr int kBlocks = 148 * kPerSm;    // also the number of partial sums
 
 // The tensors of a launch; of three sizes, since an argument is copied at every launch.
 template <int N>
@@ -49,54 +51,6 @@ __device__ __forceinline__ int tensor_of(const int32_t *chunk, int count, int c)
 
 template <typename T> struct Wide { static constexpr int kN = 16 / (int)sizeof(T); T v[kN]; };
 
-// Values [0, n) of a chunk that starts at `in`, as a thread holds them: kUnroll times 16 bytes, the loads all under way at once; zeros
-// behind the end.
-template <typename T>
-__device__ __forceinline__ void load_chunk(const T *in, int n, Wide<T> (&w)[kUnroll]) {
-    constexpr int kWide = Wide<T>::kN;
-    if ((reinterpret_cast<uintptr_t>(in) & 15u) == 0) {
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int at = (u * kThreads + threadIdx.x) * kWide;
-            if (at + kWide <= n) {
-                const uint4 raw = *reinterpret_cast<const uint4 *>(in + at);
-                memcpy(&w[u], &raw, 16);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kWide; ++i) w[u].v[i] = at + i < n ? in[at + i] : T(0.f);
-            }
-        }
-    } else {                             // any address: neighbours read neighbours
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-            for (int i = 0; i < kWide; ++i) {
-                const int at = (u * kWide + i) * kThreads + threadIdx.x;
-                w[u].v[i] = at < n ? in[at] : T(0.f);
-            }
-    }
-}
-// The same values to `out`, which the chunk was loaded for: the way back is the way of the load.
-template <typename T>
-__device__ __forceinline__ void store_chunk(T *out, int n, const Wide<T> (&w)[kUnroll], bool wide) {
-    constexpr int kWide = Wide<T>::kN;
-    const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int at = (u * kThreads + threadIdx.x) * kWide;
-        if (wide && aligned && at + kWide <= n) {
-            uint4 raw;
-            memcpy(&raw, &w[u], 16);
-            *reinterpret_cast<uint4 *>(out + at) = raw;
-        } else {
-#pragma unroll
-            for (int i = 0; i < kWide; ++i) {
-                const int one = wide ? at + i : (u * kWide + i) * kThreads + (int)threadIdx.x;
-                if (one < n) out[one] = w[u].v[i];
-            }
-        }
-    }
-}
 __device__ __forceinline__ float as_number(float x) { return x; }
 __device__ __forceinline__ double as_number(double x) { return x; }
 __device__ __forceinline__ float as_number(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -161,19 +115,73 @@ struct Scale {
     }
 };
 
-template <typename T, typename Number>
-__device__ __forceinline__ void scale_values(Wide<T> (&w)[kUnroll], const Scale<Number> &s) {
-    if (!s.scales) return;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-        for (int i = 0; i < Wide<T>::kN; ++i) w[u].v[i] = (T)(as_number(w[u].v[i]) * s.factor);
-}
 template <typename T>
 using NumberOf = std::conditional_t<sizeof(T) == 8, double, float>;
 
+__device__ __forceinline__ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// A chunk's sum of squares, this thread's share: kUnroll 16-byte loads under way at once, and the values behind the last whole 16 bytes one
+// by one; at an address that is no multiple of 16 all of them.
 template <typename T, int N>
-__global__ void __launch_bounds__(kThreads) clip_sum(const __grid_constant__ Table<N> t, double *__restrict__ partial) {
+__device__ __forceinline__ double chunk_squares(const Chunk<T, N> &c) {
+    constexpr int kWide = Wide<T>::kN;
+    double sum = 0.0;
+    int rest = 0;
+    if (aligned16(c.in)) {
+        uint4 raw[kUnroll];
+        rest = c.n / kWide * kWide;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int at = (u * kThreads + threadIdx.x) * kWide;
+            raw[u] = at < rest ? *reinterpret_cast<const uint4 *>(c.in + at) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            Wide<T> w;
+            memcpy(&w, &raw[u], 16);
+            sum += squares(w.v);
+        }
+    }
+#pragma unroll 4
+    for (int i = rest + threadIdx.x; i < c.n; i += kThreads) {
+        const T one[1] = {c.in[i]};
+        sum += squares(one);
+    }
+    return sum;
+}
+template <typename T, int N>
+__device__ __forceinline__ void scale_chunk(const Chunk<T, N> &c, const Scale<NumberOf<T>> &s) {
+    constexpr int kWide = Wide<T>::kN;
+    if (!s.scales && c.out == c.in) return;
+    int rest = 0;
+    if (aligned16(c.in) && aligned16(c.out)) {
+        uint4 raw[kUnroll];
+        rest = c.n / kWide * kWide;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int at = (u * kThreads + threadIdx.x) * kWide;
+            if (at < rest) raw[u] = *reinterpret_cast<const uint4 *>(c.in + at);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int at = (u * kThreads + threadIdx.x) * kWide;
+            if (at >= rest) break;
+            if (s.scales) {
+                Wide<T> w;
+                memcpy(&w, &raw[u], 16);
+#pragma unroll
+                for (int i = 0; i < kWide; ++i) w.v[i] = (T)(as_number(w.v[i]) * s.factor);
+                memcpy(&raw[u], &w, 16);
+            }
+            *reinterpret_cast<uint4 *>(c.out + at) = raw[u];
+        }
+    }
+#pragma unroll 4
+    for (int i = rest + threadIdx.x; i < c.n; i += kThreads) c.out[i] = s.scales ? (T)(as_number(c.in[i]) * s.factor) : c.in[i];
+}
+
+template <typename T, int N>
+__global__ void __launch_bounds__(kThreads, kPerSm) clip_sum(const __grid_constant__ Table<N> t, double *__restrict__ partial) {
     __shared__ double warp_sums[kThreads / 32];
     __shared__ int32_t chunk[N + 1];
     for (int i = threadIdx.x; i <= t.count; i += kThreads) chunk[i] = t.chunk[i];
@@ -181,20 +189,14 @@ __global__ void __launch_bounds__(kThreads) clip_sum(const __grid_constant__ Tab
     after_last_kernel();
     double sum = 0.0;
     const int chunks = chunk[t.count];
-    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const Chunk<T, N> at(t, chunk, c);
-        Wide<T> w[kUnroll];
-        load_chunk(at.in, at.n, w);
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) sum += squares(w[u].v);
-    }
+    for (int c = blockIdx.x; c < chunks; c += gridDim.x) sum += chunk_squares(Chunk<T, N>(t, chunk, c));
     sum = block_sum(sum, warp_sums);
     if (threadIdx.x == 0) partial[t.first + blockIdx.x] = sum;
     start_next_kernel();
 }
 
 template <typename T, int N>
-__global__ void __launch_bounds__(kThreads) clip_scale(const __grid_constant__ Table<N> t, const double *__restrict__ partial, double max_norm,
+__global__ void __launch_bounds__(kThreads, kScalePerSm) clip_scale(const __grid_constant__ Table<N> t, const double *__restrict__ partial, double max_norm,
                                                        void *norm_out) {
     __shared__ double warp_sums[kThreads / 32];
     __shared__ int32_t chunk[N + 1];
@@ -206,14 +208,7 @@ __global__ void __launch_bounds__(kThreads) clip_scale(const __grid_constant__ T
     for (int i = threadIdx.x; i < t.blocks; i += kThreads) sum += partial[i];
     const Scale<NumberOf<T>> s(block_sum(sum, warp_sums), max_norm);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *static_cast<NumberOf<T> *>(norm_out) = (NumberOf<T>)s.norm;
-    for (int c = chunk[t.count] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-        const Chunk<T, N> at(t, chunk, c);
-        if (!s.scales && at.out == at.in) continue;
-        Wide<T> w[kUnroll];
-        load_chunk(at.in, at.n, w);
-        scale_values(w, s);
-        store_chunk(at.out, at.n, w, (reinterpret_cast<uintptr_t>(at.in) & 15u) == 0);
-    }
+    for (int c = chunk[t.count] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) scale_chunk(Chunk<T, N>(t, chunk, c), s);
 }
 
 // Few values: one cluster does both steps, its blocks telling each other their sums through shared memory -- one launch, no scratch.
@@ -230,13 +225,7 @@ __global__ void __cluster_dims__(kCluster) __launch_bounds__(kThreads) clip_few(
     start_next_kernel();
     const int chunks = chunk[t.count];
     double sum = 0.0;
-    Wide<T> w[kUnroll];
-    for (int c = blockIdx.x; c < chunks; c += kCluster) {
-        const Chunk<T, N> at(t, chunk, c);
-        load_chunk(at.in, at.n, w);
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) sum += squares(w[u].v);
-    }
+    for (int c = blockIdx.x; c < chunks; c += kCluster) sum += chunk_squares(Chunk<T, N>(t, chunk, c));
     sum = block_sum(sum, warp_sums);
     if (threadIdx.x < kCluster) {
         uint32_t there;
@@ -249,13 +238,7 @@ __global__ void __cluster_dims__(kCluster) __launch_bounds__(kThreads) clip_few(
     for (int b = 0; b < kCluster; ++b) sum += sums[b];
     const Scale<NumberOf<T>> s(sum, max_norm);
     if (blockIdx.x == 0 && threadIdx.x == 0) *static_cast<NumberOf<T> *>(norm_out) = (NumberOf<T>)s.norm;
-    for (int c = blockIdx.x; c < chunks; c += kCluster) {
-        const Chunk<T, N> at(t, chunk, c);
-        if (!s.scales && at.out == at.in) continue;
-        if (chunks > kCluster) load_chunk(at.in, at.n, w);             // else the values are still here
-        scale_values(w, s);
-        store_chunk(at.out, at.n, w, (reinterpret_cast<uintptr_t>(at.in) & 15u) == 0);
-    }
+    for (int c = blockIdx.x; c < chunks; c += kCluster) scale_chunk(Chunk<T, N>(t, chunk, c), s);
 }
 
 template <typename T, int N>
@@ -299,7 +282,7 @@ const_status_t run(int count, const void *const *in, void *const *out, const int
     t.blocks = sums;
     for (int b = batches - 1; b >= 0 && e == cudaSuccess; --b) {       // the last batch is the one that L2 still holds
         const int blocks = fill(b);
-        CB_LAUNCH("clip_scale", stream, e = launch_early(clip_scale<T, N>, blocks, kThreads, 0, stream, t, (const double *)partial, max_norm, b == 0 ? norm : nullptr));
+        CB_LAUNCH("clip_scale", stream, e = launch_early(clip_scale<T, N>, std::min(blocks, 148 * kScalePerSm), kThreads, 0, stream, t, (const double *)partial, max_norm, b == 0 ? norm : nullptr));
     }
     if (cudaFreeAsync(partial, stream) != cudaSuccess || e != cudaSuccess) return CONST_ERR_CUDA;
     return CONST_OK;
