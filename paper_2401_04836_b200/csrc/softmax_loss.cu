@@ -531,7 +531,8 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     const int leaf = p.order - 1;
     const bool table = grad && p.grad[leaf];
     p.tensor = p.rank <= kTensorRank;
-    const int own = p.tensor ? kTensorRows : kTile, other = p.tensor ? tensor_tile(p.rank, kWide) : kTile, blocks = p.tensor ? 148 : 148 * 2;
+    const int terms_h = kWide || p.order > 2 ? 2 : 1, terms_c = kWide ? 2 : 1;
+    const int own = p.tensor ? kTensorRows : kTile, other = p.tensor ? tensor_tile(p.rank, terms_h, terms_c) : kTile, blocks = p.tensor ? 148 : 148 * 2;
     const Split by_rows = split_units(p.fibres, own, p.columns, other, blocks);
     const Split by_columns = split_units(p.columns, own, p.fibres, other, blocks);
     const int columns = image_columns(p.rank), width = p.tensor ? columns : (p.rank + kTile - 1) / kTile * kTile;
@@ -564,9 +565,9 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
         }
         if (p.tensor) {
             image_h.hi = need.take<uint16_t>(padded * columns);
-            image_h.lo = need.take<uint16_t>(padded * columns);
+            if (terms_h == 2) image_h.lo = need.take<uint16_t>(padded * columns);
             image_c.hi = need.take<uint16_t>(image_rows(p.columns) * columns);
-            if (kWide) image_c.lo = need.take<uint16_t>(image_rows(p.columns) * columns);     // bf16 has 8 bits: fp16 holds them
+            if (terms_c == 2) image_c.lo = need.take<uint16_t>(image_rows(p.columns) * columns);    // bf16 has 8 bits: fp16 holds them
         }
         const int64_t nr = by_rows.groups * by_rows.parts * by_rows.rows, nc = table ? by_columns.groups * by_columns.parts * by_columns.rows : 0;
         rows = Parts{by_rows, need.take<float>(grad ? nr * width : 0), need.take<float>(nr), need.take<float>(nr), width};
@@ -594,7 +595,7 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
             const TensorArgs a{turned ? image_c : image_h, turned ? image_h : image_c, turned ? p.columns : p.fibres, turned ? p.fibres : p.columns, columns, 0,
                                p.base, p.pull, p.words, turned ? kMaxC : kMaxH, turned ? kMaxH : kMaxC, p.words + kGaveUp,
                                knobs.spin_limit ? knobs.spin_limit : 1 << 20, knobs.withhold, s.groups, s.tiles, s.each, s.parts, to.sum, to.top, to.total, to.width};
-            CB_LAUNCH("loss_tensor", stream, ok(tensor_pass(which, kWide, a, runs_of_units, stream)));
+            CB_LAUNCH("loss_tensor", stream, ok(tensor_pass(which, terms_h, terms_c, a, runs_of_units, stream)));
         } else {
             const FlatArgs a{turned ? p.factor[leaf] : p.h, turned ? p.h : p.factor[leaf], turned ? p.columns : p.fibres, turned ? p.fibres : p.columns, p.rank,
                              p.base, p.pull, to};

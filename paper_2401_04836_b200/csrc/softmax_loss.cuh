@@ -121,11 +121,11 @@ struct Problem {
     float *base, *pull;                                // [fibres] w_f p_fk = pull_f 2^(s_fk / ln 2 + base_f)
 };
 
-// softmax_tensor.cu: rows of a group and of a tile, and one pass.  `wide`: factors in fp32 (three products a product, shares of
-// 22 bits), else in bf16 (shares of 11 bits).
+// softmax_tensor.cu: one pass, and the rows of its groups and tiles.  terms_h, terms_c: fp16 terms of rows and table.  fp32 factors have
+// two of each, and their shares have two; a table in bf16 has one, which is exact, and so have rows that are no product.
 constexpr int kTensorRows = 256;                // own rows of a group
-int tensor_tile(int rank, bool wide);           // other rows of a tile
-cudaError_t tensor_pass(int pass, bool wide, const TensorArgs &a, int blocks, cudaStream_t stream);
+int tensor_tile(int rank, int terms_h, int terms_c);    // other rows of a tile
+cudaError_t tensor_pass(int pass, int terms_h, int terms_c, const TensorArgs &a, int blocks, cudaStream_t stream);
 
 }  // namespace loss
 }  // namespace cb
