@@ -279,6 +279,9 @@ const_status_t const_execute(const_plan_t *plan, const const_operand_t *operands
  * are held in fp32; bf16 gradients are rounded once at the end.  Scores that are not finite make the losses of their rows,
  * and the gradients that these rows reach, not finite.  Gradients are added up with atomic adds, so they can differ in the
  * last bits between runs; losses do not, except of fibres with more than 64 leaves.
+ * Up to rank 128 the scores are made on the tensor cores (fp32 factors as two fp16 terms, 22 bits; shares of the gradient
+ * likewise, in bf16 of one term), above and for few scores on the fp32 pipes.  A bounded device-side wait that gives up makes
+ * every loss and gradient NaN.
  * Scratch comes from the library's pool as for const_execute (rows, their weights, partial sums; no array of the size
  * fibres x extent); without it the call returns CONST_ERR_CUDA and has written nothing.  Asynchronous on `stream`, no host
  * synchronisation; may be captured into a graph.  The current device has to be the tensor's.
@@ -369,13 +372,14 @@ const char *const_status_string(const_status_t status);
 
 /*
  * Test hook for the bounded device-side waits (the look-back of the radix sort, the chunk wait of the splitter sort, the mbarrier
- * wait of the tensor-core stage).  what = 0: number of polls after which a wait gives up (0 restores the defaults);
+ * waits of the tensor-core stage and of the softmax loss).  what = 0: number of polls after which a wait gives up (0 restores the defaults);
  * what = 1: value != 0 withholds the signal those waits wait for -- sort tiles do not publish their
- * counts or chunks, the tensor-core stage issues and commits nothing -- so that every such wait runs out, the
+ * counts or chunks, the tensor-core stage and the softmax loss issue and commit nothing -- so that every such wait runs out, the
  * kernel records CONST_ERR_TIMEOUT, skips its stores and returns normally;
  * what = 2: which of the tile shapes a launcher keeps for measurement is launched (0: the default; the
  * two-contraction network has variants 1..5, every one of them computes the same result, and 6, its matrix form alone: the
- * result stays zero where that form hands the work on);
+ * result stays zero where that form hands the work on; const_softmax_loss has 1, the fp32 pipes, and 2, the tensor cores, for any
+ * size);
  * what = 3: value != 0 makes every request of const_execute for optional scratch (padded factors, the intermediate of the
  * two-contraction network's matrix form), and of const_csf_build for the splitter sort's, fail for want of memory, so that the
  * path that needs none (less) runs;

@@ -530,7 +530,11 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     constexpr bool kWide = sizeof(T) == sizeof(float);
     const int leaf = p.order - 1;
     const bool table = grad && p.grad[leaf];
-    p.tensor = p.rank <= kTensorRank;
+    // The fp32 pipes where the scores (in tiles of kTile rows) are so few that making the images takes longer than the tensor cores save
+    // (one fibre of 12 400 to 19 us against 18 to 21; with a gradient 1000 x 200 at rank 8: 31 against 35, 500 x 2000 at rank 16: 39 against 35).
+    const double work = (double)((p.fibres + kTile - 1) / kTile * kTile) * (double)p.columns * p.rank;
+    const int variant = debug_knobs().variant;
+    p.tensor = p.rank <= kTensorRank && variant != 1 && (variant == 2 || work > (grad ? 4e6 : 3e7));
     const int terms_h = kWide || p.order > 2 ? 2 : 1, terms_c = kWide ? 2 : 1;
     const int own = p.tensor ? kTensorRows : kTile, other = p.tensor ? tensor_tile(p.rank, terms_h, terms_c) : kTile, blocks = p.tensor ? 148 : 148 * 2;
     const Split by_rows = split_units(p.fibres, own, p.columns, other, blocks);
@@ -615,7 +619,7 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     if (table) pass(kByColumns, cols);
     if (grad) {
         int64_t most = 0;
-        for (int l = 0; l <= leaf; ++l) most = std::max(most, p.extent[l] * p.rank);
+        for (int l = 0; l <= leaf; ++l) most = std::max(most, kWide && l < leaf ? 1 : p.extent[l] * p.rank);
         auto finish = [&](auto kernel, int64_t threads) {
             CB_LAUNCH("loss_finish", stream, ok(launch_early(kernel, blocks_for(threads, kThreads), kThreads, 0, stream, p, cols)));
         };

@@ -12,6 +12,14 @@ pytestmark = pytest.mark.gpu
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
+@pytest.fixture(autouse=True, params=["by size", "tensor cores", "fp32 pipes"])
+def path(request):
+    """Which kernels make the scores (the tensor cores' take ranks up to 128): as chosen by size, and each for every size."""
+    cb.const_debug_set(2, {"by size": 0, "tensor cores": 2, "fp32 pipes": 1}[request.param])
+    yield request.param
+    cb.const_debug_set(2, 0)
+
+
 class Case:
     """A random tensor of `nnz` distinct nonzeros (at most) with factors whose scores spread by about `spread`."""
 
@@ -121,6 +129,54 @@ def test_fibres_with_many_leaves():
 def test_long_vocabulary_few_rows():
     Case((7, 60_001), 32, 9).run().check()
     Case((3, 50_021), 150, 4).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rank", [24, 50, 100])
+@pytest.mark.parametrize("rows,vocabulary", [(60_001, 333), (390, 40_003)])
+def test_many_groups_and_tiles(rows, vocabulary, rank, dtype, path):
+    """Several groups of rows a block, groups cut between blocks, a last group with one tile of rows."""
+    if path == "by size":
+        pytest.skip("the tensor cores' kernels, which are tested by name")
+    Case((rows, vocabulary), rank, rows, dtype=dtype).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rank", [12, 40, 100])
+@pytest.mark.parametrize("falling", [False, True])
+def test_scores_that_grow_along_the_leaf_mode(rank, dtype, falling):
+    """Every tile of the leaf mode has larger scores than all before it, by more than a share may exceed its base; or smaller ones."""
+    c = Case((300, 3001), rank, 400, dtype=dtype)
+    ramp = torch.linspace(0.02, 25.0, 3001, device="cuda")
+    c.factors[1] = (c.factors[1].float() * (ramp.flip(0) if falling else ramp)[:, None]).to(TYPES[dtype])
+    c.run().check()
+
+
+def test_the_same_call_gives_the_same_losses():
+    c = Case((40, 30, 3000), 20, 900)
+    h = c.handle()
+    first = c.run(handle=h).loss.clone()
+    for _ in range(3):
+        assert torch.equal(c.run(handle=h).loss, first)
+
+
+def test_waits_that_give_up(path):
+    """The products are withheld: every wait for them runs out, losses and gradients become NaN, and the next call is unharmed."""
+    for rank in (12, 40, 100):
+        c = Case((200, 300), rank, 150)
+        h = c.handle()
+        cb.const_debug_set(0, 200)
+        cb.const_debug_set(1, 1)
+        try:
+            for grads in (True, None):
+                c.run(grads=grads, handle=h)
+                torch.cuda.synchronize()
+                if path == "tensor cores":
+                    assert all(torch.isnan(t).all() for t in (c.loss, *(c.grads or [])))
+        finally:
+            cb.const_debug_set(1, 0)
+            cb.const_debug_set(0, 0)
+        c.run(handle=h).check()
 
 
 def test_many_rows():
