@@ -440,12 +440,15 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
     start_next_kernel();
 }
 
-// N values at once, N = 4 where rows are multiples of 4 (and so 16-byte aligned in fp32).
+// N values at once: 4 where rows are multiples of 4 (and so 16-byte aligned in fp32), or 2.
 template <int N>
 __device__ __forceinline__ void load_values(const float *from, float (&v)[N]) {
     if constexpr (N == 4) {
         const float4 x = *reinterpret_cast<const float4 *>(from);
         v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+    } else if constexpr (N == 2) {
+        const float2 x = *reinterpret_cast<const float2 *>(from);
+        v[0] = x.x, v[1] = x.y;
     } else {
         v[0] = *from;
     }
@@ -453,6 +456,7 @@ __device__ __forceinline__ void load_values(const float *from, float (&v)[N]) {
 template <int N>
 __device__ __forceinline__ void store_values(float *to, const float (&v)[N]) {
     if constexpr (N == 4) *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    else if constexpr (N == 2) *reinterpret_cast<float2 *>(to) = make_float2(v[0], v[1]);
     else *to = v[0];
 }
 template <int N>
@@ -460,6 +464,8 @@ __device__ __forceinline__ void store_values(__nv_bfloat16 *to, const float (&v)
     if constexpr (N == 4) {
         const __nv_bfloat162 x[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
         *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(x);
+    } else if constexpr (N == 2) {
+        *reinterpret_cast<__nv_bfloat162 *>(to) = __floats2bfloat162_rn(v[0], v[1]);
     } else {
         *to = __float2bfloat16_rn(v[0]);
     }
@@ -624,11 +630,11 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
             CB_LAUNCH("loss_finish", stream, ok(launch_early(kernel, blocks_for(threads, kThreads), kThreads, 0, stream, p, cols)));
         };
         // many parts (a short leaf mode, many fibres): a warp for each value (200 rows of 123 parts at rank 8: 30 us with a thread each)
-        const int64_t values = p.rank % 4 == 0 ? most / 4 : most;
+        const int at_once = p.rank % 4 == 0 ? 4 : p.rank % 2 == 0 ? 2 : 1;
         if (table && by_columns.parts > 16)
-            p.rank % 4 == 0 ? finish(loss_finish<T, 4, true>, values * kWarp) : finish(loss_finish<T, 1, true>, values * kWarp);
+            finish(at_once == 4 ? loss_finish<T, 4, true> : at_once == 2 ? loss_finish<T, 2, true> : loss_finish<T, 1, true>, most / at_once * kWarp);
         else
-            p.rank % 4 == 0 ? finish(loss_finish<T, 4, false>, values) : finish(loss_finish<T, 1, false>, values);
+            finish(at_once == 4 ? loss_finish<T, 4, false> : at_once == 2 ? loss_finish<T, 2, false> : loss_finish<T, 1, false>, most / at_once);
     }
     ok(cudaFreeAsync(base, stream));
     return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
