@@ -277,7 +277,7 @@ const_status_t const_execute(const_plan_t *plan, const const_operand_t *operands
  *                 is overwritten with the gradient of scale * sum_f loss_f.  No two of them, nor one of them and a factor, overlap.
  * The scores are never stored: they are made tile by tile, twice where there is a gradient.  Scores, maxima, sums and gradients
  * are held in fp32; bf16 gradients are rounded once at the end.  Scores that are not finite make the losses of their rows,
- * and the gradients that these rows reach, not finite.  Gradients are added up with atomic adds, so they can differ in the
+ * and the gradients that these rows reach, not finite; so can scores beyond 1e7 in magnitude, of which fp32 holds no fractions.  Gradients are added up with atomic adds, so they can differ in the
  * last bits between runs; losses do not, except of fibres with more than 64 leaves.
  * Up to rank 128 the scores are made on the tensor cores (fp32 factors as two fp16 terms, 22 bits; shares of the gradient
  * likewise, in bf16 of one term), above and for few scores on the fp32 pipes.  A bounded device-side wait that gives up makes

@@ -347,7 +347,8 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                     for (int j = 0; j < 16; ++j)
                         if (16 * c + j < valid) m = fmaxf(m, __uint_as_float(s[j]));
                 }
-                float now = fmaxf(top, ceilf(m * unit) + (kSums && top == -INFINITY ? kRoom : 0.f));
+                // rounded up, so that no score of the tile exceeds it, however large: after a raise a tile's shares fit
+                float now = fmaxf(top, ceilf(__fmul_ru(m, unit)) + (kSums && top == -INFINITY ? kRoom : 0.f));
                 if (kPaired && kSums) {
                     told[t][h][in_tile] = now;
                     asm volatile("bar.sync %0, 256;" :: "r"(1 + t) : "memory");
@@ -466,14 +467,15 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                     asm volatile("bar.sync %0, %1;" :: "r"(barrier), "n"(kSync) : "memory");
                     ok = *(volatile int *)&chain_gave_up[chain][beat & 1] == 0;        // the same for the whole chain
                 } else if (!kSums) {
-                    bool low = i == 0;
+                    bool low = i == 0, raised;
                     float part;
 #pragma unroll 1
                     do {
+                        raised = low;
                         if (low) raise(from, valid);
                         part = shares(from, valid, vec);
                         low = __any_sync(0xffffffffu, part > 0x1p100f);
-                    } while (low);
+                    } while (low && !raised);                        // once is enough
                     total += part;
                     fence_before();
                     if (!ok) *(volatile int *)&chain_gave_up[chain][beat & 1] = 1;
@@ -486,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_tensor(const __grid_constant
                     tmem_stored();
                     fence_before();
                     if (!ok) *(volatile int *)&chain_gave_up[chain][beat & 1] = 1;
-                    low = any_of<kSync>(barrier, part > kMostShares);
+                    low = any_of<kSync>(barrier, !low && part > kMostShares);          // (to raise it once is enough)
                     ok = *(volatile int *)&chain_gave_up[chain][beat & 1] == 0;
                     fresh = !low;
                     if (low && ok) {                                 // a share of the chain was too large: its scores once more, for a higher base

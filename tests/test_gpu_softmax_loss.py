@@ -102,10 +102,21 @@ def test_weights(weights, rank):
 
 
 @pytest.mark.parametrize("rank", [12, 150])
-@pytest.mark.parametrize("spread", [0.0, 0.01, 30.0, 300.0])
+@pytest.mark.parametrize("spread", [0.0, 0.01, 30.0, 300.0, 30_000.0])
 def test_spread_of_the_scores(spread, rank):
     """All scores equal, and scores so far apart that one coordinate has all the probability."""
     Case((60, 20, 700), rank, 1500, spread=spread).run().check()
+
+
+@pytest.mark.parametrize("rank", [12, 40, 100])
+def test_scores_too_large_to_mean_anything_end(rank):
+    """A base that fp32 cannot hold to a whole power of two is raised once a tile at most."""
+    for spread in (1e9, 1e20, 1e37):
+        c = Case((200, 700), rank, 300, spread=spread)
+        c.run()
+        c.run(grads=None)
+    torch.cuda.synchronize()
+    Case((60, 20, 700), rank, 1500).run().check()
 
 
 @pytest.mark.parametrize("size", [1e-12, 1e-3, 1e4, 1e12])
