@@ -274,7 +274,8 @@ const_status_t const_execute(const_plan_t *plan, const const_operand_t *operands
  *   factors_dev   one per mode (not per level), row-major [extent of the mode][rank], CONST_F32 or CONST_BF16 (factor_dtype);
  *   loss_dev      float, one per fibre (const_csf_level(order - 2) says how many), overwritten;
  *   grads_dev     NULL: the loss alone.  Else one per mode, each NULL (not wanted) or an array like that factor, which
- *                 is overwritten with the gradient of scale * sum_f loss_f.  No two of them, nor one of them and a factor, overlap.
+ *                 is overwritten with the gradient of scale * sum_f loss_f.  No two of them and loss_dev, nor one of them and a
+ *                 factor, overlap.
  * The scores are never stored: they are made tile by tile, twice where there is a gradient.  Scores, maxima, sums and gradients
  * are held in fp32; bf16 gradients are rounded once at the end.  Scores that are not finite make the losses of their rows,
  * and the gradients that these rows reach, not finite; so can scores beyond 1e7 in magnitude, of which fp32 holds no fractions.  Gradients are added up with atomic adds, so they can differ in the
@@ -285,8 +286,8 @@ const_status_t const_execute(const_plan_t *plan, const const_operand_t *operands
  * Scratch comes from the library's pool as for const_execute (rows, their weights, partial sums; no array of the size
  * fibres x extent); without it the call returns CONST_ERR_CUDA and has written nothing.  Asynchronous on `stream`, no host
  * synchronisation; may be captured into a graph.  The current device has to be the tensor's.
- * CONST_ERR_INVALID_ARG: null or not 16-byte aligned pointers, a csf or a type other than these, rank < 1, a scale that is
- * not finite.  CONST_ERR_UNSUPPORTED: rank > 1024.
+ * CONST_ERR_INVALID_ARG: null or not 16-byte aligned pointers (loss_dev: 4-byte), results that overlap, a csf or a type other than
+ * these, rank < 1, a scale that is not finite in fp32, another current device.  CONST_ERR_UNSUPPORTED: rank > 1024.
  */
 const_status_t const_softmax_loss(const const_csf_t *csf, const void *const *factors_dev, int rank, const_dtype_t factor_dtype,
                                   double scale, void *loss_dev, void *const *grads_dev, void *stream);

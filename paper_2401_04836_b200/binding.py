@@ -418,6 +418,11 @@ def const_execute(plan: PlanHandle, operands: Dict[str, Union[CsfHandle, "object
 _torch_dtypes = None
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
 def _dtype_of(tensor, types) -> int:
     global _torch_dtypes
     if _torch_dtypes is None:
@@ -441,21 +446,22 @@ def const_softmax_loss(csf: CsfHandle, factors, loss, grads=None, scale: float =
         raise ValueError("factors and grads must have one entry per mode")
     kind = _dtype_of(factors[0], (F32, BF16))
     rank = int(factors[0].shape[-1])
+    device = _current_device()
     for m, f in enumerate(factors):
         for what, t in (("factor", f), ("gradient", None if grads is None else grads[m])):
             if t is None and what == "gradient":
                 continue
-            if not t.is_cuda or not t.is_contiguous() or t.dtype != factors[0].dtype or tuple(t.shape) != (csf.dims[m], rank):
-                raise ValueError(f"{what} {m} must be a contiguous {factors[0].dtype} CUDA tensor of shape {(csf.dims[m], rank)}")
+            if t.get_device() != device or not t.is_contiguous() or t.dtype != factors[0].dtype or tuple(t.shape) != (csf.dims[m], rank):
+                raise ValueError(f"{what} {m} must be a contiguous {factors[0].dtype} CUDA tensor of shape {(csf.dims[m], rank)} on the current device")
     n = ctypes.c_int64()
     _check(lib.const_csf_level(csf.ptr, order - 2, None, None, ctypes.byref(n)), "const_csf_level")
-    if not loss.is_cuda or not loss.is_contiguous() or _dtype_of(loss, (F32,)) != F32 or loss.numel() != n.value:
-        raise ValueError(f"loss must be a contiguous float32 CUDA tensor of {n.value} entries, one a fibre")
+    if loss.get_device() != device or not loss.is_contiguous() or _dtype_of(loss, (F32,)) != F32 or loss.numel() != n.value:
+        raise ValueError(f"loss must be a contiguous float32 CUDA tensor of {n.value} entries, one a fibre, on the current device")
     if n.value == 0 and grads is None:
         return
     ptrs = (ctypes.c_void_p * order)(*[f.data_ptr() for f in factors])
     outs = None if grads is None else (ctypes.c_void_p * order)(*[None if g is None else g.data_ptr() for g in grads])
-    at = loss.data_ptr() if n.value else factors[0].data_ptr()          # torch gives an empty tensor no address; nothing is written there
+    at = loss.data_ptr() if n.value else factors[0].data_ptr()          # torch gives an empty tensor no address; it has no bytes
     _check(lib.const_softmax_loss(csf.ptr, ptrs, rank, kind, float(scale), at, outs, _stream_int(stream)), "const_softmax_loss")
 
 
@@ -483,15 +489,18 @@ def const_clip_gradients(grads, max_norm: float, norm, out=None, stream=None) ->
     kind = F32
     if n:
         types, devices = set(map(dtype_of, tensors)), set(map(get_device, tensors))
-        if len(types) != 1 or len(devices) != 1 or min(devices) < 0 or not all(map(is_contiguous, tensors)):
-            raise ValueError("gradients (and out) must be contiguous CUDA tensors of one type on one device")
+        if len(types) != 1 or devices != {_current_device()} or not all(map(is_contiguous, tensors)):
+            raise ValueError("gradients (and out) must be contiguous CUDA tensors of one type on the current device")
         kind = _dtype_of(grads[0], (F32, F64, BF16))
     sizes = list(map(numel, grads))
     if out is not None and list(map(numel, out)) != sizes:
         raise ValueError("out must hold tensors like the gradients")
-    if norm.get_device() < 0 or norm.numel() != 1 or norm.dtype != (float64 if kind == F64 else float32):
+    if norm.get_device() != _current_device() or norm.numel() != 1 or norm.dtype != (float64 if kind == F64 else float32):
         raise ValueError("norm must be a CUDA tensor of one float32 (float64 for float64 gradients)")
     ptrs, counts = array("Q", map(data_ptr, tensors)), array("q", sizes)
+    written = [p for p in ptrs[-n:] if p] if n else []                 # an empty tensor has no address
+    if len(set(written)) != len(written):
+        raise ValueError("no two results may be the same tensor")
     at = ptrs.buffer_info()[0]
     _check(lib.const_clip_gradients(n, at, None if out is None else at + 8 * n, counts.buffer_info()[0], kind, max_norm, norm.data_ptr(),
                                     _stream_int(stream)), "const_clip_gradients")

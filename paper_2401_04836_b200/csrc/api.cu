@@ -379,13 +379,26 @@ const_status_t const_softmax_loss(const const_csf_t *h, const void *const *facto
     if (!c || !factors_dev || !loss_dev || (factor_dtype != CONST_F32 && factor_dtype != CONST_BF16) || c->dtype != CONST_F32 || rank < 1 ||
         !std::isfinite((float)scale))
         return CONST_ERR_INVALID_ARG;
-    if (!aligned16(loss_dev)) return CONST_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(loss_dev) % sizeof(float)) return CONST_ERR_INVALID_ARG;
+    // what is written overlaps nothing else: gradients are cleared before the factors are read
+    struct Range { uintptr_t at; uint64_t bytes; };
+    Range written[kMaxOrder + 1], read[kMaxOrder];
+    int n_written = 0;
+    written[n_written++] = {reinterpret_cast<uintptr_t>(loss_dev), sizeof(float) * (uint64_t)c->n[c->order - 2]};
     for (int m = 0; m < c->order; ++m) {
+        const uint64_t bytes = (uint64_t)c->dims[m] * rank * (factor_dtype == CONST_F32 ? 4 : 2);
         if (!factors_dev[m] || !aligned16(factors_dev[m])) return CONST_ERR_INVALID_ARG;
+        read[m] = {reinterpret_cast<uintptr_t>(factors_dev[m]), bytes};
         if (!grads_dev || !grads_dev[m]) continue;
         if (!aligned16(grads_dev[m])) return CONST_ERR_INVALID_ARG;
-        for (int o = 0; o < c->order; ++o)                      // a gradient is cleared before the factors are read
-            if (grads_dev[m] == factors_dev[o] || (o != m && grads_dev[m] == grads_dev[o])) return CONST_ERR_INVALID_ARG;
+        written[n_written++] = {reinterpret_cast<uintptr_t>(grads_dev[m]), bytes};
+    }
+    auto meet = [](const Range &x, const Range &y) { return x.at < y.at + y.bytes && y.at < x.at + x.bytes; };
+    for (int i = 0; i < n_written; ++i) {
+        for (int m = 0; m < c->order; ++m)
+            if (meet(written[i], read[m])) return CONST_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (meet(written[i], written[j])) return CONST_ERR_INVALID_ARG;
     }
     if (rank > kMaxLossRank) return CONST_ERR_UNSUPPORTED;
     int dev = 0;

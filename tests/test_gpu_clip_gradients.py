@@ -129,6 +129,10 @@ def test_refusals():
             cb.const_clip_gradients(*args)
     with pytest.raises(ValueError):
         cb.const_clip_gradients(grads, 1.0, norm, out=grads[:1])
+    with pytest.raises(ValueError):                                     # it would be scaled twice
+        cb.const_clip_gradients([grads[0], grads[0]], 1.0, norm)
+    out = [torch.empty_like(grads[0]) for _ in range(2)]
+    assert abs(float(clip([grads[0], grads[0]], 1e9, out)) / float(clip(grads[:1], 1e9, out[:1])) - 2 ** 0.5) < 1e-6
     with pytest.raises(ValueError):
         cb.const_clip_gradients(grads, 1.0, norm, out=[grads[0], torch.empty(21, device="cuda")])
 

@@ -346,10 +346,20 @@ def test_refusals():
         cb.const_softmax_loss(h, c.factors, loss[:-1])
     with pytest.raises(ValueError):
         cb.const_softmax_loss(h, c.factors, loss.double())
+    with pytest.raises(ValueError):
+        cb.const_softmax_loss(h, [f.cpu() for f in c.factors], loss)
+    with pytest.raises(ValueError):
+        cb.const_softmax_loss(h, c.factors, loss, grads=[grads[0], grads[1].cpu(), grads[2]])
     for bad in ([c.factors[0], grads[1], grads[2]], [grads[0], grads[1], c.factors[2]]):
         with pytest.raises(cb.ConstError) as e:                         # a gradient in a factor's place
             cb.const_softmax_loss(h, c.factors, loss, grads=bad)
         assert e.value.status == 1
+    flat = torch.zeros(12_000, device="cuda")
+    for at in (0, 4, 5996):                                             # results that overlap
+        with pytest.raises(cb.ConstError) as e:
+            cb.const_softmax_loss(h, c.factors, loss, grads=[None, flat[at:at + 600].view(30, 20), flat[:6000].view(300, 20)])
+        assert e.value.status == 1
+    cb.const_softmax_loss(h, c.factors, flat[6601:6601 + c.fibres], grads=[None, flat[6000:6600].view(30, 20), flat[:6000].view(300, 20)])
     for scale in (float("nan"), float("inf"), 1e60):
         with pytest.raises(cb.ConstError):
             cb.const_softmax_loss(h, c.factors, loss, scale=scale)
