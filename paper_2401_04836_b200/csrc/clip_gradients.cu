@@ -3,8 +3,10 @@
 // Bound by memory: every value is read for the norm, and read again and written for the scaling.  The scaling starts with the
 // values that the norm read last, so that what still lies in L2 (126 MB) is not fetched again; in place and below the limit
 // it is skipped.
-// Squares are added in fp32 over the 16 bytes .. 64 bytes a thread loads at once and in fp64 from there on, every sum in an
-// order that only the sizes decide: the same call gives the same bits.
+// Squares are added in fp32 over the 16 bytes of one load and in fp64 from there on, every sum in an order that only the sizes decide:
+// the same call gives the same bits.
+// Measured: 489 M fp32 values 0.95 ms, three passes over them at the measured copy rate 0.90; 60 M bf16 values in 300 tensors 62 us
+// (the second reading partly from L2; read and written once 37); 4 800 values 4.4 us, one launch.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -17,8 +19,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostTensors = 768;        // of a launch: their table is a kernel argument (32 KB at most)
 constexpr int kUnroll = 4;               // 16-byte loads a thread has under way
-constexpr int kPerSm = 4;                // blocks of the sum on an SM; and of the scaling (489 M fp32 values: 3 take 665 us, 4 715, 6 743: fewer
-constexpr int kScalePerSm = 3;           // streams of reads and writes at once)
+// Blocks on an SM of the sum, and of the scaling, which wants fewer streams of reads and writes at once (489 M fp32 values:
+// 3 blocks take 665 us, 4 take 715, 6 take 743).
+constexpr int kPerSm = 4, kScalePerSm = 3;
 constexpr int kBlocks = 148 * kPerSm;    // also the number of partial sums
 
 // The tensors of a launch; of three sizes, since an argument is copied at every launch.
@@ -213,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, kScalePerSm) clip_scale(const __grid
 
 // Few values: one cluster does both steps, its blocks telling each other their sums through shared memory -- one launch, no scratch.
 constexpr int kCluster = 8;
-constexpr int kClusterChunks = 4 * kCluster;           // up to so many chunks (131 072 fp32 values); 19 MB take longer than on all SMs
+constexpr int kClusterChunks = 4 * kCluster;           // up to so many chunks: 131 072 fp32 values (4 800 values: 4.4 us, 6.5 as two launches)
 
 template <typename T, int N>
 __global__ void __cluster_dims__(kCluster) __launch_bounds__(kThreads) clip_few(const __grid_constant__ Table<N> t, double max_norm, void *norm_out) {
@@ -264,7 +267,9 @@ const_status_t run(int count, const void *const *in, void *const *out, const int
         fill(0);
         if (t.chunk[t.count] <= kClusterChunks) {
             CB_LAUNCH("clip_few", stream, e = launch_early(clip_few<T, N>, kCluster, kThreads, 0, stream, t, max_norm, norm));
-            return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
+            if (e == cudaSuccess) return CONST_OK;
+            (void)cudaGetLastError();                                  // the next launch must not find this error
+            return CONST_ERR_CUDA;
         }
     }
     double *partial = nullptr;
@@ -284,8 +289,9 @@ const_status_t run(int count, const void *const *in, void *const *out, const int
         const int blocks = fill(b);
         CB_LAUNCH("clip_scale", stream, e = launch_early(clip_scale<T, N>, std::min(blocks, 148 * kScalePerSm), kThreads, 0, stream, t, (const double *)partial, max_norm, b == 0 ? norm : nullptr));
     }
-    if (cudaFreeAsync(partial, stream) != cudaSuccess || e != cudaSuccess) return CONST_ERR_CUDA;
-    return CONST_OK;
+    if (cudaFreeAsync(partial, stream) == cudaSuccess && e == cudaSuccess) return CONST_OK;
+    (void)cudaGetLastError();
+    return CONST_ERR_CUDA;
 }
 
 }  // namespace

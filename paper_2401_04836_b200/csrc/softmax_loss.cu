@@ -637,7 +637,9 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
             finish(at_once == 4 ? loss_finish<T, 4, false> : at_once == 2 ? loss_finish<T, 2, false> : loss_finish<T, 1, false>, most / at_once);
     }
     ok(cudaFreeAsync(base, stream));
-    return e == cudaSuccess ? CONST_OK : CONST_ERR_CUDA;
+    if (e == cudaSuccess) return CONST_OK;
+    (void)cudaGetLastError();                                          // the next launch must not find this error
+    return CONST_ERR_CUDA;
 }
 
 template <typename T>
