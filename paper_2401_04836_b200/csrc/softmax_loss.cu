@@ -14,27 +14,40 @@ namespace {
 constexpr int kWarp = 32;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / kWarp;
-constexpr int kRun = 64;           // leaves of a fibre that one warp walks
-constexpr int kStrip = 128;        // columns of a row that a warp holds at once, 4 a lane
+constexpr int kRun = 64;           // leaves of a fibre that one group walks
+// Rows and leaves are the work of groups of G lanes, 4 columns of a row a lane: 8 lanes up to rank 32 (15 700 fibres
+// at rank 8: a step of 40 us, with whole warps 57), else a warp.
+constexpr int kNarrowRank = 32;
 
 __device__ __forceinline__ float value(const float *p, int64_t i) { return __ldg(p + i); }
 __device__ __forceinline__ float value(const __nv_bfloat16 *p, int64_t i) { return __bfloat162float(p[i]); }
 
-__device__ __forceinline__ float warp_sum(float v) {
+// The lanes of this thread's group, for the shuffles that only they take part in.
+template <int G>
+__device__ __forceinline__ uint32_t group_mask() { return G == kWarp ? 0xffffffffu : ((1u << (G % kWarp)) - 1) << (threadIdx.x % kWarp / G * G); }
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor_sync(group_mask<G>(), v, o);
+    return v;
+}
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(group_mask<G>(), v, o));
     return v;
 }
 
 // The last p in [0, n) with pos[p] <= at (pos ascends; every node has a child, so it is the node that holds `at`).  For a whole
-// warp: every step asks at 32 places, so a range of 32 000 nodes takes three loads one after another.
+// group: every step asks at G places, so with a warp a range of 32 000 nodes takes three loads one after another.
+template <int G>
 __device__ __forceinline__ int32_t holder(const int32_t *__restrict__ pos, int64_t n, int64_t at) {
-    const int lane = threadIdx.x % kWarp;
+    const int lane = threadIdx.x % G;
     int64_t lo = 0;                                                    // pos[lo] <= at, and the answer is below lo + n
     while (n > 1) {
-        const int64_t step = (n + kWarp) / (kWarp + 1), p = lo + (lane + 1) * step;
+        const int64_t step = (n + G) / (G + 1), p = lo + (lane + 1) * step;
         const bool below = p < lo + n && __ldg(pos + p) <= at;
-        const int64_t up = step * __popc(__ballot_sync(0xffffffffu, below));
+        const int64_t up = step * __popc(__ballot_sync(group_mask<G>(), below) & group_mask<G>());
         lo += up;
         n = min(step, n - up);
     }
@@ -66,11 +79,12 @@ __device__ __forceinline__ float row_value(const Problem &p, const int32_t *at, 
     return h;
 }
 
+template <int G>
 __device__ __forceinline__ void path_of(const Problem &p, int64_t f, int32_t *at) {
     int64_t node = f;
     for (int l = p.order - 2; l >= 0; --l) {
         at[l] = __ldg(p.crd[l] + node);
-        if (l > 0) node = holder(p.pos[l], p.nodes[l - 1], node);
+        if (l > 0) node = holder<G>(p.pos[l], p.nodes[l - 1], node);
     }
 }
 
@@ -90,32 +104,33 @@ __device__ __forceinline__ void keep_largest(uint32_t *word, float v) {
     __syncthreads();
 }
 
-// One warp, at most kRun leaves [first, last) of fibre f with path `at`: weight, target scores and, with a gradient, the targets'
+// One group, at most kRun leaves [first, last) of fibre f with path `at`: weight, target scores and, with a gradient, the targets'
 // share of it.  All leaves' rows are independent loads; sums leave the registers once.
-template <typename T>
+template <typename T, int G>
 __device__ __forceinline__ void walk_leaves(const Problem &p, const int32_t *at, int64_t f, int64_t first, int64_t last, bool grad) {
-    const int lane = threadIdx.x % kWarp, leaf = p.order - 1;
+    const int lane = threadIdx.x % G, leaf = p.order - 1;
+    const uint32_t mask = group_mask<G>();
     const T *table = static_cast<const T *>(p.factor[leaf]);
     float *d_table = grad ? p.acc[leaf] : nullptr;
-    for (int strip = 0; strip < p.rank; strip += kStrip) {
+    for (int strip = 0; strip < p.rank; strip += 4 * G) {
         float h[4], sum[4] = {0.f, 0.f, 0.f, 0.f}, score = 0.f, weight = 0.f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int r = strip + lane + kWarp * q;
+            const int r = strip + lane + G * q;
             h[q] = r < p.rank ? row_value<T>(p, at, r) : 0.f;
         }
-        for (int64_t some = first; some < last; some += kWarp) {
-            const int n = (int)min(last - some, (int64_t)kWarp);
+        for (int64_t some = first; some < last; some += G) {
+            const int n = (int)min(last - some, (int64_t)G);
             const float my_x = lane < n ? __ldg(p.x + some + lane) : 0.f;
             const int32_t my_k = lane < n ? __ldg(p.crd[leaf] + some + lane) : 0;
             weight += my_x;
 #pragma unroll 4
             for (int e = 0; e < n; ++e) {
-                const float x = __shfl_sync(0xffffffffu, my_x, e);
-                const int64_t row = (int64_t)__shfl_sync(0xffffffffu, my_k, e) * p.rank;
+                const float x = __shfl_sync(mask, my_x, e, G);
+                const int64_t row = (int64_t)__shfl_sync(mask, my_k, e, G) * p.rank;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int r = strip + lane + kWarp * q;
+                    const int r = strip + lane + G * q;
                     if (r >= p.rank) continue;
                     const float c = value(table, row + r);
                     score = fmaf(x * h[q], c, score);
@@ -124,8 +139,8 @@ __device__ __forceinline__ void walk_leaves(const Problem &p, const int32_t *at,
                 }
             }
         }
-        score = warp_sum(score);
-        weight = warp_sum(weight);
+        score = group_sum<G>(score);
+        weight = group_sum<G>(weight);
         if (lane == 0) {
             atomicAdd(p.xs + f, score);
             if (strip == 0) atomicAdd(p.weight + f, weight);
@@ -133,53 +148,54 @@ __device__ __forceinline__ void walk_leaves(const Problem &p, const int32_t *at,
         if (grad)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int r = strip + lane + kWarp * q;
+                const int r = strip + lane + G * q;
                 if (r < p.rank) atomicAdd(p.xc + f * p.rank + r, sum[q]);
             }
     }
 }
 
-// One warp a fibre: its path, its row h (of which it returns the largest magnitude) and its first kRun leaves.
-template <typename T>
+// One group a fibre: its path, its row h (of which it returns the largest magnitude) and its first kRun leaves.
+template <typename T, int G>
 __device__ __forceinline__ float make_row(const Problem &p, int64_t f, bool grad, float most) {
-    const int lane = threadIdx.x % kWarp;
+    const int lane = threadIdx.x % G;
     const int32_t *__restrict__ ends = p.pos[p.order - 1];
     const int64_t first = __ldg(ends + f), last = __ldg(ends + f + 1);
     int32_t at[kMaxOrder - 1];
-    path_of(p, f, at);
+    path_of<G>(p, f, at);
     for (int l = 0; l + 1 < p.order; ++l)
         if (lane == l) p.path[l][f] = at[l];
-    for (int r = lane; r < p.rank; r += kWarp) {
+    for (int r = lane; r < p.rank; r += G) {
         const float h = row_value<T>(p, at, r);
         p.h[f * p.rank + r] = h;
         most = larger_finite(most, h);
     }
-    walk_leaves<T>(p, at, f, first, min(last, first + kRun), grad);
+    walk_leaves<T, G>(p, at, f, first, min(last, first + kRun), grad);
     return most;
 }
 
-// One warp a run of kRun leaves: those among them that are not the first kRun of their fibre.  They can only be of the fibre that
+// One group a run of kRun leaves: those among them that are not the first kRun of their fibre.  They can only be of the fibre that
 // holds the run's first leaf.
-template <typename T>
+template <typename T, int G>
 __device__ __forceinline__ void walk_run(const Problem &p, int64_t run, bool grad) {
     const int32_t *__restrict__ ends = p.pos[p.order - 1];
-    const int64_t f = holder(ends, p.fibres, run), first = max(run, (int64_t)__ldg(ends + f) + kRun), last = min(run + kRun, (int64_t)__ldg(ends + f + 1));
+    const int64_t f = holder<G>(ends, p.fibres, run), first = max(run, (int64_t)__ldg(ends + f) + kRun), last = min(run + kRun, (int64_t)__ldg(ends + f + 1));
     if (first >= last) return;
     int32_t at[kMaxOrder - 1];
-    path_of(p, f, at);
-    walk_leaves<T>(p, at, f, first, last, grad);
+    path_of<G>(p, f, at);
+    walk_leaves<T, G>(p, at, f, first, last, grad);
 }
 
-template <typename T>
+template <typename T, int G>
 __global__ void __launch_bounds__(kThreads) loss_prepare(const __grid_constant__ Problem p, bool grad) {
     after_last_kernel();
-    const int64_t warps = (int64_t)gridDim.x * kWarps, me = (int64_t)blockIdx.x * kWarps + threadIdx.x / kWarp;
+    const int64_t groups = (int64_t)gridDim.x * (kThreads / G), me = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
     const int64_t runs = (p.leaves + kRun - 1) / kRun;
     float most_h = 0.f, most_c = 0.f;
-    for (int64_t i = me; i < p.fibres + runs; i += warps) {
-        if (i < p.fibres) most_h = make_row<T>(p, i, grad, most_h);
-        else walk_run<T>(p, (i - p.fibres) * kRun, grad);
+    for (int64_t i = me; i < p.fibres + runs; i += groups) {
+        if (i < p.fibres) most_h = make_row<T, G>(p, i, grad, most_h);
+        else walk_run<T, G>(p, (i - p.fibres) * kRun, grad);
     }
+    __syncwarp();
     if (p.tensor) {
         const T *table = static_cast<const T *>(p.factor[p.order - 1]);
         const int64_t n = p.columns * p.rank, all = (int64_t)gridDim.x * kThreads;
@@ -361,17 +377,19 @@ __global__ void __launch_bounds__(kThreads) loss_flat(const __grid_constant__ Fl
 // joining the parts
 // ------------------------------------------------------------------------------------------------
 
-// The loss of every fibre, and with a gradient dh scattered to the factors above the leaves.  TEAM warps of a block have a fibre: one,
-// or all where there are many parts a fibre (few fibres, a long leaf mode).
-template <typename T, int TEAM>
+// The loss of every fibre, and with a gradient dh scattered to the factors above the leaves.  A fibre is the work of a group of G lanes; or
+// of all warps of a block (TEAM) where there are many parts a fibre (few fibres, a long leaf mode).
+template <typename T, int TEAM, int G>
 __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Problem p, const __grid_constant__ Parts parts, bool grad) {
-    __shared__ float shared_top[kWarps], shared_total[kWarps], shared_sum[TEAM > 1 ? kWarps : 1][kWarp];
+    static_assert(TEAM == 1 || (TEAM == kWarps && G == kWarp));
+    constexpr int kFibres = kThreads / G / TEAM;                       // of a block at once
+    __shared__ float shared_top[kWarps], shared_total[kWarps], shared_sum[TEAM > 1 ? kWarps : 1][4][kWarp];
     after_last_kernel();
-    const int lane = threadIdx.x % kWarp, warp = threadIdx.x / kWarp, member = warp % TEAM;
+    const int lane = threadIdx.x % G, member = threadIdx.x / G % TEAM;
     const bool gave_up = p.words[kGaveUp] != 0;
     const float pull = p.tensor ? exp2f((float)image_exponent(p.words[kMaxWeight])) : 1.f;
-    const int64_t step = (int64_t)gridDim.x * (kWarps / TEAM);
-    for (int64_t f = (int64_t)blockIdx.x * (kWarps / TEAM) + warp / TEAM; f < p.fibres; f += step) {
+    const int64_t step = (int64_t)gridDim.x * kFibres;
+    for (int64_t f = (int64_t)blockIdx.x * kFibres + threadIdx.x / G / TEAM; f < p.fibres; f += step) {
         const int64_t g = f / parts.split.rows, row = f - g * parts.split.rows, first = g * parts.split.parts;
         const int n = parts.split.parts_of(g);
         const float w = p.weight[f], score = p.xs[f];
@@ -379,24 +397,23 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
         for (int l = 0; l + 1 < p.order; ++l) at[l] = grad ? p.path[l][f] : 0;
         const float *tops = parts.top + first * parts.split.rows + row, *totals = parts.total + first * parts.split.rows + row;
         float top = -INFINITY, total = 0.f;
-        for (int s = member * kWarp + lane; s < n; s += TEAM * kWarp) top = fmaxf(top, tops[(int64_t)s * parts.split.rows]);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int s = member * G + lane; s < n; s += TEAM * G) top = fmaxf(top, tops[(int64_t)s * parts.split.rows]);
+        top = group_max<G>(top);
         if (TEAM > 1) {
-            if (lane == 0) shared_top[warp] = top;
+            if (lane == 0) shared_top[member] = top;
             __syncthreads();
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, shared_top[w]);
+            for (int o = 0; o < TEAM; ++o) top = fmaxf(top, shared_top[o]);
         }
-        for (int s = member * kWarp + lane; s < n; s += TEAM * kWarp) {
+        for (int s = member * G + lane; s < n; s += TEAM * G) {
             const float t = tops[(int64_t)s * parts.split.rows];
             total += totals[(int64_t)s * parts.split.rows] * (t == top ? 1.f : exp2f(t - top));
         }
-        total = warp_sum(total);
+        total = group_sum<G>(total);
         if (TEAM > 1) {
-            if (lane == 0) shared_total[warp] = total;
+            if (lane == 0) shared_total[member] = total;
             __syncthreads();
             total = 0.f;
-            for (int w = 0; w < kWarps; ++w) total += shared_total[w];
+            for (int o = 0; o < TEAM; ++o) total += shared_total[o];
         }
         if (gave_up) total = NAN;
         if (lane == 0 && member == 0) {
@@ -405,26 +422,32 @@ __global__ void __launch_bounds__(kThreads) loss_rows(const __grid_constant__ Pr
         }
         if (grad) {
             const float share = w / total;
-            for (int r0 = 0; r0 < p.rank; r0 += kWarp) {
-                const int r = r0 + lane;
-                float sum = 0.f;
-                if (r < p.rank) {
-#pragma unroll 4
-                    for (int s = member; s < n; s += TEAM) {
-                        const float t = tops[(int64_t)s * parts.split.rows];
-                        sum = fmaf(parts.sum[((first + s) * parts.split.rows + row) * parts.width + r], t == top ? 1.f : exp2f(t - top), sum);
-                    }
+            for (int r0 = 0; r0 < p.rank; r0 += 4 * G) {
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+                for (int s = member; s < n; s += TEAM) {
+                    const float t = tops[(int64_t)s * parts.split.rows], keep = t == top ? 1.f : exp2f(t - top);
+                    const float *from = parts.sum + ((first + s) * parts.split.rows + row) * parts.width + r0 + lane;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (r0 + lane + G * q < p.rank) sum[q] = fmaf(from[G * q], keep, sum[q]);
                 }
                 if (TEAM > 1) {
-                    shared_sum[warp][lane] = sum;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) shared_sum[member % (TEAM > 1 ? kWarps : 1)][q][lane] = sum[q];
                     __syncthreads();
-                    sum = 0.f;
-                    for (int o = 0; o < kWarps; ++o) sum += shared_sum[o % TEAM][lane];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        sum[q] = 0.f;
+                        for (int o = 0; o < TEAM; ++o) sum[q] += shared_sum[o][q][lane];
+                    }
                 }
-                // the factors' rows are dealt to the members
-                if (r < p.rank) {
-                    const float dh = p.scale * (share * sum - p.xc[f * p.rank + r]);
-                    for (int l = member; l + 1 < p.order; l += TEAM) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = r0 + lane + G * q;
+                    if (r >= p.rank) continue;
+                    const float dh = p.scale * (share * sum[q] - p.xc[f * p.rank + r]);
+                    for (int l = member; l + 1 < p.order; l += TEAM) {       // the factors' rows are dealt to the members
                         if (!p.acc[l]) continue;
                         float d = dh;
                         for (int m = 0; m + 1 < p.order; ++m)
@@ -497,7 +520,7 @@ __global__ void __launch_bounds__(kThreads) loss_finish(const __grid_constant__ 
             }
             if (MANY)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] = warp_sum(sum[i]);
+                for (int i = 0; i < N; ++i) sum[i] = group_sum<kWarp>(sum[i]);
             if (member) continue;
             load_values<N>(p.acc[leaf] + e * N, part);
 #pragma unroll
@@ -593,7 +616,11 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     for (int64_t n : zero.n) zeros += n;
     CB_LAUNCH("loss_clear", stream, ok(launch_early(loss_clear, blocks_for(zeros, 4 * kThreads), kThreads, 0, stream, zero)));
     const int64_t runs = (p.leaves + kRun - 1) / kRun, values = p.tensor ? p.columns * p.rank / 32 : 0;
-    CB_LAUNCH("loss_prepare", stream, ok(launch_early(loss_prepare<T>, blocks_for(std::max(p.fibres + runs, values / kWarp), kWarps), kThreads, 0, stream, p, grad)));
+    const bool narrow = p.rank <= kNarrowRank;
+    const int64_t pieces = std::max(p.fibres + runs, values / kWarp);
+    CB_LAUNCH("loss_prepare", stream,
+              ok(narrow ? launch_early(loss_prepare<T, 8>, blocks_for(pieces, kThreads / 8), kThreads, 0, stream, p, grad)
+                        : launch_early(loss_prepare<T, kWarp>, blocks_for(pieces, kWarps), kThreads, 0, stream, p, grad)));
     if (p.tensor)
         CB_LAUNCH("loss_images", stream, ok(launch_early(loss_images<T>, blocks_for((padded + image_rows(p.columns)) * (columns / 8), kThreads), kThreads, 0, stream, p, image_h, image_c)));
     auto pass = [&](int which, const Parts &to) {
@@ -618,10 +645,10 @@ const_status_t run(Problem p, bool grad, cudaStream_t stream) {
     };
     pass(grad ? kByRows : kLossAlone, rows);
     // many parts a fibre: a block for each (77 fibres of 148 parts, rank 64: 67 us with a warp each)
-    if (by_rows.parts > 16)
-        CB_LAUNCH("loss_rows", stream, ok(launch_early(loss_rows<T, kWarps>, blocks_for(p.fibres, 1), kThreads, 0, stream, p, rows, grad)));
-    else
-        CB_LAUNCH("loss_rows", stream, ok(launch_early(loss_rows<T, 1>, blocks_for(p.fibres, kWarps), kThreads, 0, stream, p, rows, grad)));
+    CB_LAUNCH("loss_rows", stream,
+              ok(by_rows.parts > 16 ? launch_early(loss_rows<T, kWarps, kWarp>, blocks_for(p.fibres, 1), kThreads, 0, stream, p, rows, grad)
+                 : narrow           ? launch_early(loss_rows<T, 1, 8>, blocks_for(p.fibres, kThreads / 8), kThreads, 0, stream, p, rows, grad)
+                                    : launch_early(loss_rows<T, 1, kWarp>, blocks_for(p.fibres, kWarps), kThreads, 0, stream, p, rows, grad)));
     if (table) pass(kByColumns, cols);
     if (grad) {
         int64_t most = 0;
