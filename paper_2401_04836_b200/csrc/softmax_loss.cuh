@@ -118,6 +118,7 @@ struct Problem {
     float *xs, *weight;                                // [fibres] sum_leaves x s, sum_leaves x
     uint32_t *words;                                   // kWords
     bool tensor;                                       // the passes run on the tensor cores: pull is scaled as the images are
+    bool short_loss;                                   // a loss alone of so few leaves that one group has all of a fibre's: nothing is added up, nothing cleared
     float *base, *pull;                                // [fibres] w_f p_fk = pull_f 2^(s_fk / ln 2 + base_f)
 };
 

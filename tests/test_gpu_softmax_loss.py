@@ -228,6 +228,17 @@ def test_values_of_rows_that_no_leaf_reaches_are_not_read():
     c.check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rank", [7, 40, 300])
+@pytest.mark.parametrize("leaves", [1, 9, 63, 64, 65, 130])
+@pytest.mark.parametrize("rows", [1, 60])
+def test_the_loss_alone_of_few_leaves(rows, leaves, rank, dtype):
+    Case((80, 400), 40, 3000).run(grads=False)                           # what it leaves in the scratch memory must not matter
+    c = Case((rows, 333), rank, leaves, dtype=dtype, weights="uniform")
+    for _ in range(2):
+        c.run(grads=False).check()
+
+
 def test_a_row_that_is_not_finite_stays_alone():
     c = Case((200, 300), 20, 150).run().check()
     loss, bound = c.loss.clone(), to_dev(c.expected()[0][1])
