@@ -222,6 +222,8 @@ template <typename T, int N>
 __global__ void __cluster_dims__(kCluster) __launch_bounds__(kThreads) clip_few(const __grid_constant__ Table<N> t, double max_norm, void *norm_out) {
     __shared__ double warp_sums[kThreads / 32], sums[kCluster];
     __shared__ int32_t chunk[N + 1];
+    // a block's shared memory is written by others only once that block runs: waited for below, behind the sum
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;");
     for (int i = threadIdx.x; i <= t.count; i += kThreads) chunk[i] = t.chunk[i];
     __syncthreads();
     after_last_kernel();
@@ -230,11 +232,13 @@ __global__ void __cluster_dims__(kCluster) __launch_bounds__(kThreads) clip_few(
     double sum = 0.0;
     for (int c = blockIdx.x; c < chunks; c += kCluster) sum += chunk_squares(Chunk<T, N>(t, chunk, c));
     sum = block_sum(sum, warp_sums);
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (threadIdx.x < kCluster) {
         uint32_t there;
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x])), "r"(threadIdx.x));
         asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(there), "d"(sum) : "memory");
     }
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     sum = 0.0;
 #pragma unroll
