@@ -298,8 +298,8 @@ const_status_t const_softmax_loss(const const_csf_t *csf, const void *const *fac
  * grads_dev[i] holds sizes[i] values (0 is allowed) of `dtype` (CONST_F32, CONST_F64 or CONST_BF16) at any address that is a
  * multiple of one value; 16-byte aligned ones are read and written with 128-bit accesses.  out_dev NULL, or an entry equal to that of grads_dev:
  * in place; otherwise the arrays must not overlap any other.  norm_dev receives the norm before the scaling (float; double for CONST_F64).
- * max_norm >= 0; infinity scales nothing.  A norm that is not finite scales nothing either: the values come through
- * as they are, and the caller sees the norm and drops the step.
+ * max_norm >= 0; infinity scales nothing.  A norm that is not finite in norm_dev's type scales nothing either: the values
+ * come through as they are, and the caller sees the norm and drops the step.
  * Squares are added in fp32 over at most 8 values and in fp64 above that, in an order that only the sizes decide: the same call
  * gives the same bits.  Above some 130 000 values scratch (10 KB) as for const_execute; without it CONST_ERR_CUDA.  Asynchronous on `stream`;
  * may be captured.

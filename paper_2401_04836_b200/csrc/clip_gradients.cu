@@ -106,14 +106,15 @@ struct Chunk {
     }
 };
 
-// norm and factor from a sum of squares; a norm that is no finite number scales nothing: the caller sees it and drops the step
+// norm and factor from a sum of squares; a norm that is no finite number of the type it is given in scales nothing: the caller sees
+// it and drops the step
 template <typename Number>
 struct Scale {
     double norm;
     bool scales;
     Number factor;
     __device__ __forceinline__ Scale(double sum, double max_norm) : norm(sqrt(sum)) {
-        scales = norm > max_norm && isfinite(norm);
+        scales = norm > max_norm && isfinite((Number)norm);
         factor = scales ? (Number)(max_norm / norm) : (Number)1;
     }
 };

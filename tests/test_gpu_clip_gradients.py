@@ -96,6 +96,15 @@ def test_a_norm_that_is_not_finite_scales_nothing(bad, dtype):
     assert all(torch.equal(torch.nan_to_num(a, 1.5), torch.nan_to_num(b, 1.5)) for a, b in zip(grads, out))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("count", [4, 500_000])
+def test_a_norm_above_the_largest_fp32_scales_nothing(count, dtype):
+    """Every value is finite, the norm in 64 bits too; but not in the type that the caller sees."""
+    grads = [torch.full((count,), 3e38, device="cuda", dtype=dtype), torch.ones(5, device="cuda", dtype=dtype)]
+    place = [g.clone() for g in grads]
+    assert float(clip(place, 1.0)) == float("inf") and all(torch.equal(a, b) for a, b in zip(grads, place))
+
+
 def test_the_same_call_gives_the_same_bits():
     grads = make([1_000_003, 65_537, 12], torch.float32)
     norms = {float(clip(grads, 1.0, [torch.empty_like(g) for g in grads])) for _ in range(5)}
