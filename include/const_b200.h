@@ -297,7 +297,7 @@ const_status_t const_softmax_loss(const const_csf_t *csf, const void *const *fac
  *     norm = sqrt(sum of the squares of all values of all tensors),   out = grad * min(1, max_norm / norm).
  * grads_dev[i] holds sizes[i] values (0 is allowed) of `dtype` (CONST_F32, CONST_F64 or CONST_BF16) at any address that is a
  * multiple of one value; 16-byte aligned ones are read and written with 128-bit accesses.  out_dev NULL, or an entry equal to that of grads_dev:
- * in place; otherwise the arrays must not overlap any other.  norm_dev receives the norm before the scaling (float; double for CONST_F64).
+ * in place; else no result, nor the norm, may overlap anything (CONST_ERR_INVALID_ARG).  norm_dev receives the norm before the scaling (float; double for CONST_F64).
  * max_norm >= 0; infinity scales nothing.  A norm that is not finite in norm_dev's type scales nothing either: the values
  * come through as they are, and the caller sees the norm and drops the step.
  * Squares are added in fp32 over at most 8 values and in fp64 above that, in an order that only the sizes decide: the same call

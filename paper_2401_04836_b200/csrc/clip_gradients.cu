@@ -10,6 +10,8 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <memory>
+#include <new>
 
 #include "common.cuh"
 
@@ -299,6 +301,33 @@ const_status_t run(int count, const void *const *in, void *const *out, const int
     return CONST_ERR_CUDA;
 }
 
+// Whether what is written (results, norm) meets anything else: a range of addresses sorted by its start meets an earlier one if it
+// starts before that one's end.
+const_status_t check_ranges(int count, const void *const *in, void *const *out, const int64_t *sizes, int64_t width, const void *norm, int64_t norm_bytes) {
+    struct Range { uintptr_t at, end; bool written; };
+    std::unique_ptr<Range[]> range(new (std::nothrow) Range[2 * (size_t)count + 1]);
+    if (!range) return CONST_ERR_WORKSPACE;
+    size_t n = 0;
+    auto add = [&](const void *p, int64_t bytes, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        range[n++] = {at, at + (uintptr_t)bytes, written};
+    };
+    add(norm, norm_bytes, true);
+    for (int i = 0; i < count; ++i) {
+        if (sizes[i] == 0) continue;
+        add(out[i], sizes[i] * width, true);
+        if (in[i] != out[i]) add(in[i], sizes[i] * width, false);
+    }
+    std::sort(range.get(), range.get() + n, [](const Range &a, const Range &b) { return a.at < b.at; });
+    uintptr_t end = 0, written_end = 0;
+    for (size_t i = 0; i < n; ++i) {
+        if (range[i].at < (range[i].written ? end : written_end)) return CONST_ERR_INVALID_ARG;
+        end = std::max(end, range[i].end);
+        if (range[i].written) written_end = std::max(written_end, range[i].end);
+    }
+    return CONST_OK;
+}
+
 }  // namespace
 
 const_status_t run_clip_gradients(int count, const void *const *in, void *const *out, const int64_t *sizes, const_dtype_t dtype, double max_norm,
@@ -307,6 +336,9 @@ const_status_t run_clip_gradients(int count, const void *const *in, void *const 
     int64_t total = 0;
     for (int i = 0; i < count; ++i) total += sizes[i] / 1024 + 1;
     if (total >= 2147483647ll) return CONST_ERR_UNSUPPORTED;
+    const int64_t width = dtype == CONST_F64 ? 8 : dtype == CONST_F32 ? 4 : 2;
+    const const_status_t ranges = check_ranges(count, in, out, sizes, width, norm, dtype == CONST_F64 ? 8 : 4);
+    if (ranges != CONST_OK) return ranges;
     auto sized = [&](auto one) {
         using T = decltype(one);
         if (count <= 16) return run<T, 16>(count, in, out, sizes, max_norm, norm, stream);

@@ -132,6 +132,16 @@ def test_refusals():
         with pytest.raises(cb.ConstError) as e:
             cb.const_clip_gradients(grads, norm=norm, **bad)
         assert e.value.status == 1
+    flat = torch.randn(300, device="cuda")
+    for views, out in (([flat[:200], flat[100:]], None), ([flat[:100]], [flat[50:150]]), ([flat[:100], flat[100:200]], [flat[100:200], flat[:100]])):
+        with pytest.raises(cb.ConstError) as e:
+            cb.const_clip_gradients(views, 1.0, norm, out=out)
+        assert e.value.status == 1
+    with pytest.raises(cb.ConstError):
+        cb.const_clip_gradients([flat[:100]], 1.0, flat[99:100])
+    side = torch.full((600,), 9.0, device="cuda")                        # side by side, and read twice, is no overlap
+    clip([flat[:100], flat[:100], flat[50:]], 1.0, [side[100:200], side[:100], side[200:450]])
+    assert (side[:450] != 9.0).all() and (side[450:] == 9.0).all()
     for args in (([grads[0], grads[1].double()], 1.0, norm), ([g.half() for g in grads], 1.0, norm), (grads, 1.0, norm.double()),
                  ([torch.randn(8, 8, device="cuda").t()], 1.0, norm), ([g.cpu() for g in grads], 1.0, norm)):
         with pytest.raises(ValueError):

@@ -39,6 +39,26 @@ def test_clip_gradients_refuses_before_any_device_call():
     assert run(sizes=(2 ** 45,)) == 2
 
 
+def test_clip_gradients_refuses_results_that_overlap():
+    lib = ctypes.CDLL(cb.library_path())
+    lib.const_clip_gradients.argtypes = [ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_double,
+                                         ctypes.c_void_p, ctypes.c_void_p]
+    x, y, z, norm = (BASE + 4096 * i for i in range(4))
+
+    def run(grads, out, n=8, norm=norm):
+        arrays = [(ctypes.c_void_p * len(a))(*a) if a else None for a in (grads, out)]
+        return lib.const_clip_gradients(len(grads), *arrays, (ctypes.c_int64 * len(grads))(*[n] * len(grads)), 0, 1.0, norm, None)
+
+    assert run([x, x], None) == 1                              # the same tensor in place twice
+    assert run([x, x + 4], None) == 1 and run([x + 4, x], None) == 1
+    assert run([x], [x + 4]) == 1 and run([x + 28], [x]) == 1
+    assert run([x, y], [z, z]) == 1 and run([x, y], [z + 28, z]) == 1
+    assert run([x, y], [y, x]) == 1 and run([x, y], [x, x]) == 1
+    assert run([x, x], [x, y]) == 1                            # one result replaces what another is made from
+    assert run([x], None, norm=x + 28) == 1 and run([x], [y], norm=x) == 1 and run([x], [y], norm=y + 4) == 1
+    assert run([x, y], None, n=1 << 20) == 1                   # 4 MB from each
+
+
 def test_bf16_is_no_type_of_tensors_or_plans():
     lib = cb.load_library()
     out = ctypes.c_void_p()
